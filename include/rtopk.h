@@ -279,6 +279,115 @@ typedef struct {
     } pass_rec[RTOPK_TRACE_MAX_PASSES];
 } rtopk_row_trace;
 
+/*
+ * ------------------------------------------------------------------------------------------------
+ * Operators on rows of logits, beside the selection: what a language model's rows are used for once they are there.
+ *
+ * What they have in common.  Calls enqueue on `hip_stream` (NULL = the default stream) and return without synchronising; they allocate
+ * nothing; arguments are checked on the host before anything is launched, and the status covers arguments and launches.
+ *   rows         [batch][n], element type dt, device; row r starts row_stride elements after row r - 1 (row_stride >= n), rows need no
+ *                alignment beyond the element size.  1 <= n <= RTOPK_MAX_N.
+ *   temperature  given as its inverse, positive: p_j = exp(x_j / T) / sum exp(x_l / T).  The maximum is taken off first.
+ *   masks        -inf (or the type's lowest value) takes a logit out: p = 0.  In a row where nothing but -inf is left every p is 0.  A NaN or
+ *                +inf makes every number of its row NaN, as the formulas do; the other rows are not touched by it.
+ *   arithmetic   32 bits throughout; gradients are rounded once, to the logits' type.  Sums have a fixed order: the same call gives the same bits
+ *                (rtopk_route's counts are whole numbers).
+ *   gradients    must not overlap the logits.
+ * ------------------------------------------------------------------------------------------------
+ */
+
+/*
+ * Log probabilities of given tokens, entropy, and the k best logits with theirs.
+ *
+ *   tokens           device, [batch][m] int64.  A negative one is padding: its log probability is 0 and it has no gradient.  One of n or more: NaN.
+ *   out_logprobs     device, [batch][m]: ln p of the tokens.
+ *   out_entropy      device, [batch], or NULL: - sum p ln p.
+ *   out_row_stats    device, [batch][2], or NULL: the row's maximum M and S = sum exp((x_j - M) / T), for rtopk_logprobs_backward
+ *                    (log-sum: M / T + ln S).
+ *   out_top_logprobs, out_top_indices   device, [batch][k], k >= 0: ln p and position of the k largest logits, best first, lowest index first among
+ *                    equals, in the order of rtopk_select.
+ *   workspace        device, 256-byte aligned, rtopk_logprobs_workspace_bytes() for the same batch, n, m, k and dt.
+ */
+rtopk_status rtopk_logprobs_workspace_bytes(int64_t batch, int64_t n, int64_t m, int64_t k, rtopk_dtype dt, size_t* bytes_out);
+rtopk_status rtopk_logprobs(const void* logits, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                            const int64_t* tokens, int64_t m, int64_t k, float* out_logprobs, float* out_entropy, float* out_row_stats,
+                            float* out_top_logprobs, int64_t* out_top_indices, void* workspace, size_t workspace_bytes, void* hip_stream);
+/*
+ * Its gradient: out_grad[batch][n] (type dt, rows grad_stride elements apart), d(sum grad_logprobs * logprobs + sum grad_entropy * entropy) / d logits.
+ * grad_entropy NULL: none; otherwise `entropy` is what rtopk_logprobs returned.  Tokens listed twice add up, in the order they are listed in.
+ */
+rtopk_status rtopk_logprobs_backward(const void* logits, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                                     const int64_t* tokens, int64_t m, const float* row_stats, const float* grad_logprobs, const float* entropy,
+                                     const float* grad_entropy, void* out_grad, int64_t grad_stride, void* hip_stream);
+
+/*
+ * Distillation from a teacher's top logits: per row, the divergence of the student's softmax from what is known of the teacher's.
+ *
+ *   teacher_values   device, [batch][k], type teacher_dt: the teacher's logits that were kept (rtopk_select's out_values).
+ *   teacher_columns  device, [batch][k] int64: their columns (rtopk_select's out_indices), distinct within a row.  A negative one is padding: lists may
+ *                    be shorter than k, or empty.  One of n or more makes the row's loss NaN.
+ *   teacher_lse      device, [batch], or NULL.  NULL: the teacher's distribution is the softmax over what is listed, and the loss is
+ *                        sum q_i (ln q_i - ln p_i);   an empty list has loss 0.
+ *                    Otherwise the teacher's own ln sum exp(z / T) over its whole row: q_i = exp(z_i / T - lse), and all that is not listed is one
+ *                    class more, with r = max(0, 1 - sum q_i) against the student's P = sum of p over what is not listed:  + r (ln r - ln P).
+ *   out_loss         device, [batch].
+ *   out_row_stats    device, [batch][RTOPK_DISTILL_ROW_STATS], or NULL: what rtopk_distill_backward needs of the row; the first two are the student's M
+ *                    and S as in rtopk_logprobs.
+ *   workspace        device, 256-byte aligned, rtopk_distill_workspace_bytes() for the same batch, n, k and dt.
+ * The loss is not multiplied by T^2.
+ */
+#define RTOPK_DISTILL_ROW_STATS 8
+rtopk_status rtopk_distill_workspace_bytes(int64_t batch, int64_t n, int64_t k, rtopk_dtype dt, size_t* bytes_out);
+rtopk_status rtopk_distill(const void* student, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                           const void* teacher_values, rtopk_dtype teacher_dt, const int64_t* teacher_columns, int64_t k, const float* teacher_lse,
+                           float* out_loss, float* out_row_stats, void* workspace, size_t workspace_bytes, void* hip_stream);
+/*
+ * Its gradient to the student: out_grad[batch][n] (type dt, rows grad_stride elements apart) = grad_loss[row] * d loss[row] / d student.  The lists, lse and
+ * temperature are the forward call's.  A row whose grad_loss is 0 gets zeros whatever its logits are.
+ */
+rtopk_status rtopk_distill_backward(const void* student, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                                    const void* teacher_values, rtopk_dtype teacher_dt, const int64_t* teacher_columns, int64_t k,
+                                    const float* teacher_lse, const float* row_stats, const float* grad_loss, void* out_grad, int64_t grad_stride,
+                                    void* hip_stream);
+/* Both in one call, for training loops that know the rows' weights beforehand: out_loss[batch], and the gradient of sum row_weights * loss. */
+rtopk_status rtopk_distill_step(const void* student, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                                const void* teacher_values, rtopk_dtype teacher_dt, const int64_t* teacher_columns, int64_t k,
+                                const float* teacher_lse, const float* row_weights, float* out_loss, void* out_grad, int64_t grad_stride,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Routing to experts: the k best of each token's row of experts, and their weights.
+ *
+ *   logits       device, [tokens][experts], type dt, rows row_stride elements apart; at most RTOPK_ROUTE_MAX_EXPERTS experts.
+ *   scores       softmax of the row, or sigmoids with RTOPK_ROUTE_SIGMOID (each step rounded to 32 bits).
+ *   bias         device, [experts] or NULL: added to the scores for the choice alone, not for the weights.
+ *   choice       by score + bias; without a bias (and without RTOPK_ROUTE_GROUP_TOP2) by the logits, which have the same order.  Best first, lowest
+ *                index first among equals, NaN above all.  An expert whose logit is -inf is chosen when nothing else is left, and has weight 0.
+ *   groups       the experts in `groups` groups of neighbours (groups divides experts, at most RTOPK_ROUTE_MAX_GROUPS); only the topk_groups groups
+ *                whose best choice value (RTOPK_ROUTE_GROUP_TOP2: the sum of whose two best) is highest are chosen from.  1, 1: no groups.
+ *   k            at most RTOPK_ROUTE_MAX_K and topk_groups * experts / groups.
+ *   out_weights  device, [tokens][k]: scale * score, with RTOPK_ROUTE_RENORMALIZE scale * score / (sum of the chosen scores) (0 where that sum is 0).
+ *   out_experts  device, [tokens][k] int64.
+ *   counts       device, [experts] int64, or NULL: the number of tokens that chose each expert is ADDED to it.
+ */
+enum {
+    RTOPK_ROUTE_SIGMOID = 1u << 0,
+    RTOPK_ROUTE_RENORMALIZE = 1u << 1,
+    RTOPK_ROUTE_GROUP_TOP2 = 1u << 2
+};
+#define RTOPK_ROUTE_MAX_EXPERTS 1024
+#define RTOPK_ROUTE_MAX_GROUPS 64
+#define RTOPK_ROUTE_MAX_K 64
+rtopk_status rtopk_route(const void* logits, int64_t tokens, int64_t experts, int64_t row_stride, rtopk_dtype dt, const float* bias, int64_t groups,
+                         int64_t topk_groups, int64_t k, uint32_t flags, float scale, float* out_weights, int64_t* out_experts, int64_t* counts,
+                         void* hip_stream);
+/*
+ * The weights' gradient to the logits: out_grad[tokens][experts], type dt, rows grad_stride elements apart.  `chosen` is out_experts of the forward call; flags and scale are
+ * its too.  The choice has no gradient, nor has the bias.
+ */
+rtopk_status rtopk_route_backward(const void* logits, int64_t tokens, int64_t experts, int64_t row_stride, rtopk_dtype dt, const int64_t* chosen, int64_t k,
+                                  uint32_t flags, float scale, const float* grad_weights, void* out_grad, int64_t grad_stride, void* hip_stream);
+
 /* Static description of an error code. */
 const char* rtopk_status_string(rtopk_status status);
 

@@ -32,6 +32,15 @@ EXPORTS = (
     "rtopk_select_events",
     "rtopk_select_static",
     "rtopk_select_ragged",
+    "rtopk_logprobs_workspace_bytes",
+    "rtopk_logprobs",
+    "rtopk_logprobs_backward",
+    "rtopk_distill_workspace_bytes",
+    "rtopk_distill",
+    "rtopk_distill_backward",
+    "rtopk_distill_step",
+    "rtopk_route",
+    "rtopk_route_backward",
     "rtopk_status_string",
     "rtopk_version",
 )
@@ -95,8 +104,9 @@ class RtopkError(RuntimeError):
 
 
 _SOURCES = ("rtopk_api.hip", "rtopk_f32.hip", "rtopk_f16.hip", "rtopk_bf16.hip", "rtopk_list_f32.hip", "rtopk_list_f16.hip",
-            "rtopk_list_bf16.hip", "rtopk_rows_f32.hip", "rtopk_rows_f16.hip", "rtopk_rows_bf16.hip")
-_HEADERS = ("rtopk_device.h", "rtopk_host.h", "rtopk_kernels.inl", "rtopk_sort.inl", "rtopk_list.inl")
+            "rtopk_list_bf16.hip", "rtopk_rows_f32.hip", "rtopk_rows_f16.hip", "rtopk_rows_bf16.hip",
+            "rtopk_logprobs.hip", "rtopk_distill.hip", "rtopk_route.hip")
+_HEADERS = ("rtopk_device.h", "rtopk_host.h", "rtopk_softmax.h", "rtopk_kernels.inl", "rtopk_sort.inl", "rtopk_list.inl")
 
 
 def build(force: bool = True) -> str:
@@ -163,6 +173,21 @@ def load():
         lib.rtopk_select_ragged.restype = ctypes.c_int
         lib.rtopk_select_ragged.argtypes = [vp, vp, vp, i64, i64, i64, ctypes.c_int, ctypes.c_int, u32, u64, vp, vp, vp, sz, vp,
                                             ctypes.POINTER(RtopkTuning)]
+        f32, ci = ctypes.c_float, ctypes.c_int
+        rows = [vp, i64, i64, i64, ci, f32]  # logits, batch, n, row stride, type, 1 / temperature
+        lists = rows + [vp, ci, vp, i64, vp]  # ... teacher's values, their type, columns, k, log-sum
+        for name, argtypes in (
+                ("rtopk_logprobs_workspace_bytes", [i64, i64, i64, i64, ci, ctypes.POINTER(sz)]),
+                ("rtopk_logprobs", rows + [vp, i64, i64, vp, vp, vp, vp, vp, vp, sz, vp]),
+                ("rtopk_logprobs_backward", rows + [vp, i64, vp, vp, vp, vp, vp, i64, vp]),
+                ("rtopk_distill_workspace_bytes", [i64, i64, i64, ci, ctypes.POINTER(sz)]),
+                ("rtopk_distill", lists + [vp, vp, vp, sz, vp]),
+                ("rtopk_distill_backward", lists + [vp, vp, vp, i64, vp]),
+                ("rtopk_distill_step", lists + [vp, vp, vp, i64, vp, sz, vp]),
+                ("rtopk_route", rows[:5] + [vp, i64, i64, i64, u32, f32, vp, vp, vp, vp]),
+                ("rtopk_route_backward", rows[:5] + [vp, i64, u32, f32, vp, vp, i64, vp])):
+            getattr(lib, name).restype = ctypes.c_int
+            getattr(lib, name).argtypes = argtypes
         lib.rtopk_status_string.restype = ctypes.c_char_p
         lib.rtopk_status_string.argtypes = [ctypes.c_int]
         lib.rtopk_version.restype = ctypes.c_char_p

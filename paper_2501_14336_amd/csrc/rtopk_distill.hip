@@ -1,0 +1,329 @@
+// Distillation from a teacher's top logits: the divergence of a student's row from a teacher's list of (column, logit), and its gradient
+// (rtopk_distill, rtopk_distill_backward, rtopk_distill_step).
+//
+//   q_i = exp(z_i / T) / sum exp(z_l / T), or exp(z_i / T - lse) with the teacher's own log-sum; then r = max(0, 1 - sum q) is the rest's share
+//   L   = sum q_i (ln q_i - ln p_{t_i}) [ + r (ln r - ln P),  P = sum of p over the columns that are not listed ]
+//   dL/dx_j = (1/T) [ (sum q + r) p_j - sum_{t_i = j} q_i - [j not listed] r p_j / P ]
+//
+// P is added up from the columns that are not listed, not taken as what the listed ones leave of 1: a trained student leaves 1e-6 and less.
+#include "rtopk_softmax.h"
+
+namespace rtopk {
+
+// What a row's forward pass leaves for its gradient.  p_j = exp((x_j - m) / T) / s.
+struct DistillRow {
+    float m, s;        // the student's maximum and sum
+    float zref, zmul;  // q_i = exp((z_i - zref) / T) * zmul, or exp(z_i / T - zref) with the teacher's log-sum
+    float mu, dense;   // columns not listed: dx = (g / T) exp((x - mu) / T) dense
+    float q, spare;    // sum q + r
+};
+static_assert(sizeof(DistillRow) == RTOPK_DISTILL_ROW_STATS * sizeof(float), "as declared");
+
+struct DistillParams {
+    const char* student;
+    long long row_bytes, row0, k;
+    u32 n, parts, part_vecs;
+    float c, inv_t;
+    const void* values;         // [batch][k], type value_dt
+    int value_dt;
+    const long long* columns;   // [batch][k]
+    const float* teacher_lse;   // [batch], or null
+    float4* partial;            // [batch][parts][2]: columns not listed, listed columns
+    float* loss;
+    DistillRow* rows;
+    // the gradient
+    const float* grad_loss;
+    char* grad;
+    long long grad_bytes;
+};
+
+constexpr int kDistillBlock = 256, kDistillVecs = 4;
+
+// Statistics of a part of a row; TAIL: apart for columns that are listed and for the others.
+template <int DT, bool TAIL>
+__global__ void __launch_bounds__(kDistillBlock) k_distill_part(DistillParams P) {
+    extern __shared__ u32 marks[];  // TAIL: a byte per vector of the part, a bit per column
+    __shared__ float4 sm[kDistillBlock / 64];
+    constexpr int E = RowElem<DT>::E;
+    const u32 part = blockIdx.x % P.parts;
+    const long long row = P.row0 + blockIdx.x / P.parts;
+    const RowView<DT> r(P.student, row, P.row_bytes, P.n);
+    const u32 v0 = part * P.part_vecs, v1 = part_end(v0, P.part_vecs, r.nvec);
+    SoftSum a, listed;
+    if (TAIL) {
+        const long long* columns = P.columns + row * P.k;
+        for (u32 i = threadIdx.x; i < (P.part_vecs + 3) / 4; i += kDistillBlock) marks[i] = 0;
+        __syncthreads();
+        for (long long i = threadIdx.x; i < P.k; i += kDistillBlock) {
+            const long long t = columns[i];
+            const u64 p = (u64)(t + r.lead) - (u64)v0 * E;  // (wraps below the part)
+            if (t >= 0 && t < (long long)P.n && p < (u64)(v1 - v0) * E) {
+                const u32 v = (u32)p / E, bit = 1u << ((v & 3) * 8 + (u32)p % E);
+                if (!(atomicOr(&marks[v >> 2], bit) & bit)) {  // a column listed twice counts once
+                    const float x[1] = {RowElem<DT>::load(r.x, (u32)t)};
+                    soft_add<false>(listed, x, P.c);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    sweep_vectors<DT, kDistillBlock, kDistillVecs, false>(r, v0, v1, [&](const u32x4 (&q)[kDistillVecs], u32 first) {
+        float x[kDistillVecs * E];
+#pragma unroll
+        for (int i = 0; i < kDistillVecs; ++i) {
+            float y[E];
+            RowElem<DT>::unpack(q[i], y);
+            u32 out = 0;
+            if (TAIL) {
+                const u32 v = first + i * kDistillBlock + threadIdx.x;
+                if (v < v1) out = ((const uint8_t*)marks)[v - v0];
+            }
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[i * E + j] = TAIL && ((out >> j) & 1) ? -__builtin_inff() : y[j];
+        }
+        soft_add<false>(a, x, P.c);
+    });
+    a = soft_block<kDistillBlock, false>(a, P.c, sm);
+    if (threadIdx.x == 0) P.partial[(row * P.parts + part) * 2] = packed(a);
+    if (TAIL) {
+        __syncthreads();
+        listed = soft_block<kDistillBlock, false>(listed, P.c, sm);
+        if (threadIdx.x == 0) P.partial[(row * P.parts + part) * 2 + 1] = packed(listed);
+    }
+}
+
+// ln of an entry's share.
+__device__ __forceinline__ float ln_share(float z, const DistillRow& d, bool tail, float ln_zmul, float inv_t) {
+    return tail ? z * inv_t - d.zref : (z - d.zref) * inv_t + ln_zmul;
+}
+
+constexpr int kDistillFinish = 256;
+
+template <int DT>
+__global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams P) {
+    __shared__ float4 sm[3][kDistillFinish / 64];
+    __shared__ double sums[2][kDistillFinish / 64];
+    const long long row = P.row0 + blockIdx.x;
+    const bool tail = P.teacher_lse != nullptr;
+    const RowView<DT> r(P.student, row, P.row_bytes, P.n);
+    const long long* columns = P.columns + row * P.k;
+    SoftSum a, listed, z;
+    for (u32 i = threadIdx.x; i < P.parts; i += kDistillFinish) {
+        a = soft_join<false>(a, unpacked(P.partial[(row * P.parts + i) * 2]), P.c);
+        if (tail) listed = soft_join<false>(listed, unpacked(P.partial[(row * P.parts + i) * 2 + 1]), P.c);
+    }
+    a = soft_block<kDistillFinish, false>(a, P.c, sm[0]);
+    const SoftSum others = a;
+    if (tail) a = soft_join<false>(a, soft_block<kDistillFinish, false>(listed, P.c, sm[1]), P.c);
+    DistillRow d;
+    d.m = a.m;
+    d.s = a.s;
+    d.spare = 0.0f;
+    float ln_zmul = 0.0f;
+    if (tail) {
+        d.zref = P.teacher_lse[row];
+        d.zmul = 1.0f;
+    } else {
+        for (long long i = threadIdx.x; i < P.k; i += kDistillFinish)
+            if (columns[i] >= 0) {
+                const float v[1] = {load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i))};
+                soft_add<false>(z, v, P.c);
+            }
+        z = soft_block<kDistillFinish, false>(z, P.c, sm[2]);
+        d.zref = finite_or_zero(z.m);
+        d.zmul = z.s == 0.0f ? 0.0f : 1.0f / z.s;
+        ln_zmul = z.s == 0.0f ? 0.0f : -kLn2 * log2_fast(z.s);
+    }
+    const float ln_s = kLn2 * log2_fast(a.s);
+    float loss = 0.0f;
+    double q = 0.0;  // (what is left of 1 may be a millionth: its logarithm counts)
+    for (long long i = threadIdx.x; i < P.k; i += kDistillFinish) {
+        const long long t = columns[i];
+        if (t < 0) continue;
+        const float z = load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i)), lq = ln_share(z, d, tail, ln_zmul, P.inv_t), qi = expf(lq);
+        if (tail) q += exp((double)z * (double)P.inv_t - (double)d.zref);
+        if (t >= (long long)P.n) {
+            loss += __builtin_nanf("");
+        } else if (qi != 0.0f) {
+            const float x = RowElem<DT>::load(r.x, (u32)t);
+            loss += qi * (lq - (a.s == 0.0f ? -__builtin_inff() : (x - a.m) * P.inv_t - ln_s));
+        }
+    }
+    loss = sum_block<kDistillFinish>(loss, (float*)sums[0]);
+    if (tail) {
+        q = sum_block<kDistillFinish>(q, sums[1]);
+        const float rest = q < 1.0 ? (float)(1.0 - q) : q != q ? (float)q : 0.0f;
+        const float ln_other = others.s == 0.0f ? -__builtin_inff() : (others.m - a.m) * P.inv_t + kLn2 * log2_fast(others.s) - ln_s;
+        if (rest != 0.0f) loss += rest * (kLn2 * log2_fast(rest) - ln_other);
+        d.q = q < 1.0 ? 1.0f : (float)q;
+        d.mu = finite_or_zero(others.m);
+        d.dense = others.s == 0.0f ? 0.0f : d.q * exp2_fast((d.mu - finite_or_zero(a.m)) * P.c) / a.s - rest / others.s;
+    } else {
+        d.q = z.s == 0.0f ? 0.0f : z.s != z.s ? z.s : 1.0f;
+        d.mu = finite_or_zero(a.m);
+        d.dense = a.s == 0.0f ? 0.0f : d.q / a.s;
+    }
+    if (threadIdx.x == 0) {
+        P.loss[row] = loss;
+        if (P.rows) P.rows[row] = d;
+    }
+}
+
+constexpr int kDistillGradBlock = 256, kDistillGradVecs = 4;
+
+template <int DT>
+__global__ void __launch_bounds__(kDistillGradBlock) k_distill_grad(DistillParams P) {
+    extern __shared__ u32 marks[];
+    __shared__ u32 twice;
+    const u32 part = blockIdx.x % P.parts;
+    const long long row = P.row0 + blockIdx.x / P.parts;
+    const RowView<DT> r(P.student, row, P.row_bytes, P.n);
+    char* out = P.grad + row * P.grad_bytes;
+    const bool aligned = (((uintptr_t)out ^ (uintptr_t)r.x) & 15) == 0;
+    const long long* columns = P.columns + row * P.k;
+    const u32 v0 = part * P.part_vecs, v1 = part_end(v0, P.part_vecs, r.nvec);
+    const DistillRow d = P.rows[row];
+    const float g = P.grad_loss[row] * P.inv_t, a = g * d.dense, b = d.s == 0.0f ? 0.0f : d.q / d.s, m = finite_or_zero(d.m);
+    const bool tail = P.teacher_lse != nullptr;
+    write_gradient<DT, kDistillGradBlock, kDistillGradVecs, false>(
+        r, out, aligned, v0, v1, g == 0.0f ? 0 : P.k, marks, &twice, [&](long long i) { return columns[i]; },
+        [&](long long i) {
+            const float z = load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i));
+            return expf(ln_share(z, d, tail, 0.0f, P.inv_t)) * d.zmul;
+        },
+        [&](float x) { return g == 0.0f ? 0.0f : a * exp2_fast((x - d.mu) * P.c); },
+        [&](float x, float q) { return g * (b * exp2_fast((x - m) * P.c) - q); });
+}
+
+constexpr int64_t kDistillMostVecs = (int64_t)1 << 15;  // (the bitmaps: a byte each)
+
+static RowParts distill_parts(int64_t batch, int64_t n, int eb) {
+    return deal_row(batch, n, eb, kDistillBlock * kDistillVecs, 2048, kDistillMostVecs);
+}
+
+}  // namespace rtopk
+
+using namespace rtopk;
+
+static rtopk_status check_lists(const void* student, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                                const void* teacher_values, rtopk_dtype teacher_dt, const int64_t* teacher_columns, int64_t k, const float* teacher_lse) {
+    const rtopk_status s = check_rows(student, batch, n, row_stride, dt);
+    if (s != RTOPK_OK) return s;
+    if (!usable_temperature(inv_temperature) || k < 1 || k > 0x7fffffff || !teacher_values || !teacher_columns) return RTOPK_ERR_INVALID_ARG;
+    if (teacher_dt != RTOPK_F32 && teacher_dt != RTOPK_F16 && teacher_dt != RTOPK_BF16) return RTOPK_ERR_INVALID_ARG;
+    if ((uintptr_t)teacher_columns % 8 || (uintptr_t)teacher_values % (teacher_dt == RTOPK_F32 ? 4 : 2) || (uintptr_t)teacher_lse % 4) return RTOPK_ERR_UNSUPPORTED;
+    return RTOPK_OK;
+}
+
+static DistillParams distill_params(const void* student, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature, const void* teacher_values,
+                                    rtopk_dtype teacher_dt, const int64_t* teacher_columns, int64_t k, const float* teacher_lse) {
+    DistillParams P = {};
+    P.student = (const char*)student;
+    P.row_bytes = row_stride * (dt == RTOPK_F32 ? 4 : 2);
+    P.n = (u32)n;
+    P.k = k;
+    P.c = inv_temperature * kLog2e;
+    P.inv_t = inv_temperature;
+    P.values = teacher_values;
+    P.value_dt = teacher_dt;
+    P.columns = (const long long*)teacher_columns;
+    P.teacher_lse = teacher_lse;
+    return P;
+}
+
+extern "C" {
+
+rtopk_status rtopk_distill_workspace_bytes(int64_t batch, int64_t n, int64_t k, rtopk_dtype dt, size_t* bytes_out) {
+    if (!bytes_out || batch < 1 || batch > 0x7fffffff || n < 1 || n > RTOPK_MAX_N || k < 1 || k > 0x7fffffff) return RTOPK_ERR_INVALID_ARG;
+    if (dt != RTOPK_F32 && dt != RTOPK_F16 && dt != RTOPK_BF16) return RTOPK_ERR_INVALID_ARG;
+    const int eb = dt == RTOPK_F32 ? 4 : 2;
+    *bytes_out = up256((size_t)batch * distill_parts(batch, n, eb).parts * 2 * sizeof(float4)) + up256((size_t)batch * sizeof(DistillRow));
+    return RTOPK_OK;
+}
+
+rtopk_status rtopk_distill(const void* student, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                           const void* teacher_values, rtopk_dtype teacher_dt, const int64_t* teacher_columns, int64_t k, const float* teacher_lse,
+                           float* out_loss, float* out_row_stats, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    rtopk_status s = check_lists(student, batch, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse);
+    if (s != RTOPK_OK) return s;
+    if (!out_loss || !workspace) return RTOPK_ERR_INVALID_ARG;
+    if (((uintptr_t)out_loss | (uintptr_t)out_row_stats) % 4 || (uintptr_t)workspace % 256) return RTOPK_ERR_UNSUPPORTED;
+    size_t need = 0;
+    s = rtopk_distill_workspace_bytes(batch, n, k, dt, &need);
+    if (s != RTOPK_OK) return s;
+    if (workspace_bytes < need) return RTOPK_ERR_WORKSPACE_TOO_SMALL;
+    DistillParams P = distill_params(student, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse);
+    const RowParts d = distill_parts(batch, n, dt == RTOPK_F32 ? 4 : 2);
+    P.parts = d.parts;
+    P.part_vecs = d.vecs;
+    P.partial = (float4*)workspace;
+    P.loss = out_loss;
+    P.rows = (DistillRow*)out_row_stats;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    (void)hipGetLastError();  // an error left by earlier HIP calls of the process is not this call's
+    return by_type(dt, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        const int64_t rows = kMostWorkgroups / d.parts > 0 ? kMostWorkgroups / d.parts : 1;
+        for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
+            const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
+            if (teacher_lse) hipLaunchKernelGGL((k_distill_part<DT, true>), dim3(now * d.parts), dim3(kDistillBlock), d.vecs, st, P);
+            else hipLaunchKernelGGL((k_distill_part<DT, false>), dim3(now * d.parts), dim3(kDistillBlock), 0, st, P);
+            hipLaunchKernelGGL((k_distill_finish<DT>), dim3(now), dim3(kDistillFinish), 0, st, P);
+        }
+        return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
+    });
+}
+
+rtopk_status rtopk_distill_backward(const void* student, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                                    const void* teacher_values, rtopk_dtype teacher_dt, const int64_t* teacher_columns, int64_t k,
+                                    const float* teacher_lse, const float* row_stats, const float* grad_loss, void* out_grad, int64_t grad_stride,
+                                    void* hip_stream) {
+    rtopk_status s = check_lists(student, batch, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse);
+    if (s == RTOPK_OK) s = check_rows(out_grad, batch, n, grad_stride, dt);
+    if (s != RTOPK_OK) return s;
+    const int eb = dt == RTOPK_F32 ? 4 : 2;
+    if (!row_stats || !grad_loss || rows_overlap(student, row_stride, out_grad, grad_stride, batch, n, eb)) return RTOPK_ERR_INVALID_ARG;
+    if (((uintptr_t)row_stats | (uintptr_t)grad_loss) % 4) return RTOPK_ERR_UNSUPPORTED;
+    DistillParams P = distill_params(student, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse);
+    const RowParts d = deal_row(batch, n, eb, kDistillGradBlock * kDistillGradVecs, 4096, kDistillMostVecs);
+    P.parts = d.parts;
+    P.part_vecs = d.vecs;
+    P.rows = (DistillRow*)row_stats;
+    P.grad_loss = grad_loss;
+    P.grad = (char*)out_grad;
+    P.grad_bytes = grad_stride * eb;
+    (void)hipGetLastError();
+    return by_type(dt, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        const int64_t rows = kMostWorkgroups / d.parts > 0 ? kMostWorkgroups / d.parts : 1;
+        for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
+            const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
+            hipLaunchKernelGGL((k_distill_grad<DT>), dim3(now * d.parts), dim3(kDistillGradBlock), k > 1 ? d.vecs : 0, (hipStream_t)hip_stream, P);
+        }
+        return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
+    });
+}
+
+rtopk_status rtopk_distill_step(const void* student, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
+                                const void* teacher_values, rtopk_dtype teacher_dt, const int64_t* teacher_columns, int64_t k,
+                                const float* teacher_lse, const float* row_weights, float* out_loss, void* out_grad, int64_t grad_stride,
+                                void* workspace, size_t workspace_bytes, void* hip_stream) {
+    size_t need = 0;
+    rtopk_status s = rtopk_distill_workspace_bytes(batch, n, k, dt, &need);
+    if (s != RTOPK_OK) return s;
+    if (!workspace || !out_grad || !row_weights) return RTOPK_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return RTOPK_ERR_WORKSPACE_TOO_SMALL;
+    // what can be refused is, before anything is launched
+    s = check_rows(out_grad, batch, n, grad_stride, dt);
+    if (s != RTOPK_OK) return s;
+    if ((uintptr_t)row_weights % 4) return RTOPK_ERR_UNSUPPORTED;
+    if (rows_overlap(student, row_stride, out_grad, grad_stride, batch, n, dt == RTOPK_F32 ? 4 : 2)) return RTOPK_ERR_INVALID_ARG;
+    float* rows = (float*)((char*)workspace + need - up256((size_t)batch * sizeof(DistillRow)));
+    s = rtopk_distill(student, batch, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse, out_loss, rows, workspace,
+                      workspace_bytes, hip_stream);
+    if (s != RTOPK_OK) return s;
+    return rtopk_distill_backward(student, batch, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse, rows, row_weights,
+                                  out_grad, grad_stride, hip_stream);
+}
+
+}  // extern "C"
