@@ -24,28 +24,38 @@ struct RouteParams {
     long long grad_bytes;
 };
 
-constexpr int kRouteBlock = 256;  // a wave per token
+// A token is taken by L lanes of a wave, lane l of them holding experts l N to l N + N - 1: 16 lanes up to 256 experts (four tokens to a wave: its steps across lanes are
+// moves within a row of 16, and cost the same for four tokens as for one), a whole wave beyond, or where more than 16 experts are wanted.
+template <int L, int N>
+struct RouteShape {
+    static constexpr int kTokens = 64 / L;                    // of a wave
+    static constexpr int kStage = L * N + L * N / 32 + L;     // words of LDS per token: its row with a word after every 32 (groups of 32 and 64 begin in different banks), and what was chosen
+    static constexpr u32 place(u32 e) { return e + e / 32; }  // of an expert's word
+};
 
 // 1 / (1 + e^-x) in the steps that a 32-bit program takes, each rounded: what is chosen by it is chosen alike everywhere.
 __device__ __forceinline__ float sigmoid_of(float x) { return 1.0f / (1.0f + expf(-x)); }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+// Over a token's lanes, the same in all of them: rotations within rows of 16 lanes pair the same two sums in every lane.
+template <int CTRL>
+__device__ __forceinline__ u32 row_rotated(u32 v) { return (u32)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false); }
+template <int L, class T, class Op>
+__device__ __forceinline__ T token_reduce(T v, Op&& op) {
+    auto bits = [](T x) { return __builtin_bit_cast(u32, x); };
+    auto back = [](u32 x) { return __builtin_bit_cast(T, x); };
+    v = op(v, back(row_rotated<0x128>(bits(v))));
+    v = op(v, back(row_rotated<0x124>(bits(v))));
+    v = op(v, back(row_rotated<0x122>(bits(v))));
+    v = op(v, back(row_rotated<0x121>(bits(v))));
+    if constexpr (L == 64) {
+        v = op(v, __shfl_xor(v, 16));
+        v = op(v, __shfl_xor(v, 32));
+    }
     return v;
 }
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return v;
-}
-__device__ __forceinline__ u32 wave_max_u32(u32 v) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = max(v, (u32)__shfl_xor((int)v, d));
-    return v;
-}
-
-__device__ __forceinline__ float number_of_f32_key(u32 o) { return __uint_as_float((o & 0x80000000u) ? (o ^ 0x80000000u) : ~o); }
+struct AddOf { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct FmaxOf { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct UmaxOf { __device__ __forceinline__ u32 operator()(u32 a, u32 b) const { return max(a, b); } };
 
 // What the wave's lanes wrote to LDS is there for all of them.
 __device__ __forceinline__ void wave_sync() {
@@ -54,8 +64,33 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+__device__ __forceinline__ float number_of_f32_key(u32 o) { return __uint_as_float((o & 0x80000000u) ? (o ^ 0x80000000u) : ~o); }
+
+// A lane's logits, -inf beyond the row.  `aligned`: rows start on a multiple of the lane's bytes, 16 at most.
+template <int DT, int N>
+__device__ __forceinline__ void lane_logits(const char* row, u32 first, u32 experts, bool aligned, float (&x)[N]) {
+    constexpr int kBytes = N * RowElem<DT>::kBytes, kWord = kBytes < 16 ? kBytes : 16;
+    if constexpr (kBytes >= 4) {
+        if (aligned && first + N <= experts) {
+            union { u32 w[kBytes / 4]; uint16_t h[kBytes / 2]; } q;
+#pragma unroll
+            for (int i = 0; i < kBytes / kWord; ++i) {
+                const char* p = row + (size_t)first * RowElem<DT>::kBytes + i * kWord;
+                if constexpr (kWord == 16) *(u32x4*)&q.w[i * 4] = *(const u32x4*)p;
+                else if constexpr (kWord == 8) *(uint2*)&q.w[0] = *(const uint2*)p;
+                else q.w[0] = *(const u32*)p;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] = RowElem<DT>::from_bits(DT == RTOPK_F32 ? q.w[j] : (q.w[j / 2] >> (j & 1 ? 16 : 0)) & 0xffffu);
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = first + j < experts ? RowElem<DT>::load(row, first + j) : -__builtin_inff();
+}
+
 // Scores of a lane's experts; all zero in a row without anything but -inf.
-template <int N>
+template <int L, int N>
 __device__ __forceinline__ void scores_of(const float (&x)[N], float (&s)[N], bool sigmoid) {
     if (sigmoid) {
 #pragma unroll
@@ -65,148 +100,203 @@ __device__ __forceinline__ void scores_of(const float (&x)[N], float (&s)[N], bo
     float m = x[0];
 #pragma unroll
     for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
-    m = finite_or_zero(wave_max(m));
+    m = finite_or_zero(token_reduce<L>(m, FmaxOf{}));
     float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < N; ++j) sum += s[j] = expf(x[j] - m);
-    sum = wave_sum(sum);
+    sum = token_reduce<L>(sum, AddOf{});
 #pragma unroll
     for (int j = 0; j < N; ++j) s[j] = sum == 0.0f ? 0.0f : s[j] / sum;
 }
 
-// A wave per token; lane l holds experts l N to l N + N - 1.
-template <int DT, int N>
-__global__ void __launch_bounds__(kRouteBlock) k_route(RouteParams P) {
-    __shared__ float stage[kRouteBlock / 64][64 * N];
-    const u32 lane = lane_id(), wave = threadIdx.x >> 6;
-    const long long row = P.row0 + (long long)blockIdx.x * (kRouteBlock / 64) + wave;
-    if (row >= P.tokens) return;  // (no barrier below: a wave works by itself)
-    const char* x_row = P.logits + row * P.row_bytes;
+template <int DT, int L, int N, int B>
+__global__ void __launch_bounds__(B) k_route(RouteParams P) {
+    typedef RouteShape<L, N> S;
+    __shared__ float stage[B / L][S::kStage];
+    __shared__ u32 tally[L * N];  // what this workgroup's tokens chose
+    const u32 lane = lane_id(), wave = threadIdx.x >> 6, l = lane % L, slot = threadIdx.x / L;
     const bool sigmoid = (P.flags & RTOPK_ROUTE_SIGMOID) != 0, top2 = (P.flags & RTOPK_ROUTE_GROUP_TOP2) != 0;
-    float x[N], s[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const u32 e = lane * N + j;
-        x[j] = e < P.experts ? RowElem<DT>::load(x_row, e) : -__builtin_inff();
+    constexpr u32 kWord = N * RowElem<DT>::kBytes < 16 ? N * RowElem<DT>::kBytes : 16;
+    const bool aligned = (((uintptr_t)P.logits | (uintptr_t)P.row_bytes) & (kWord - 1)) == 0;
+    if (P.counts) {
+        for (u32 i = threadIdx.x; i < P.experts; i += B) tally[i] = 0;
+        __syncthreads();
     }
-    scores_of(x, s, sigmoid);
-    u32 key[N];  // orders the choice; 0 for what may not be chosen
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const u32 e = lane * N + j;
-        float c = x[j];
-        if (x[j] != -__builtin_inff()) {
-            if (P.bias) c = s[j] + (e < P.experts ? P.bias[e] : 0.0f);
-            else if (top2) c = s[j];
-        }
-        key[j] = e < P.experts ? KeyOf<RTOPK_F32>::key(__float_as_uint(c)) : 0u;
-        if (P.groups > 1 && e < P.experts) stage[wave][e] = c;
-    }
-    if (P.groups > 1) {
-        wave_sync();
-        u32 gkey = 0;
-        if (lane < P.groups) {
-            u32 a = 0, b = 0;  // the keys of the two best
-            for (u32 i = 0; i < P.group_size; ++i) {
-                const u32 v = KeyOf<RTOPK_F32>::key(__float_as_uint(stage[wave][lane * P.group_size + i]));
-                b = max(b, min(a, v));
-                a = max(a, v);
-            }
-            const float best = number_of_f32_key(a), second = number_of_f32_key(b);
-            gkey = !top2 || b == 0 ? a : KeyOf<RTOPK_F32>::key(__float_as_uint(best + second));
-        }
-        u32 better = 0;
-        for (u32 g = 0; g < P.groups; ++g) {
-            const u32 o = (u32)__shfl((int)gkey, (int)g);
-            better += o > gkey || (o == gkey && g < lane);
-        }
-        const u64 stays = ballot64(lane < P.groups && better < P.topk_groups);
+    float* const mine = stage[slot];
+    u32* const picked = (u32*)(mine + L * N + L * N / 32);
+    for (long long first = (long long)blockIdx.x * (B / L); first < P.tokens; first += (long long)gridDim.x * (B / L)) {
+        // (lanes of a token that is none work on the last one's row, and store nothing)
+        const long long token = first + slot, row = token < P.tokens ? token : P.tokens - 1;
+        float x[N], s[N];
+        lane_logits<DT, N>(P.logits + row * P.row_bytes, l * N, P.experts, aligned, x);
+        scores_of<L, N>(x, s, sigmoid);
+        u32 key[N];  // orders the choice; 0 for what may not be chosen
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const u32 e = lane * N + j;
-            if (e < P.experts && !((stays >> (e / P.group_size)) & 1)) key[j] = 0;
-        }
-    }
-    float mine_s = 0.0f;
-    u32 mine_e = 0;
-    for (u32 r = 0; r < P.k; ++r) {
-        u32 best = key[0], at = 0;
-#pragma unroll
-        for (int j = 1; j < N; ++j)
-            if (key[j] > best) {
-                best = key[j];
-                at = j;
+            const u32 e = l * N + j;
+            float c = x[j];
+            if (x[j] != -__builtin_inff()) {
+                if (P.bias) c = s[j] + (e < P.experts ? P.bias[e] : 0.0f);
+                else if (top2) c = s[j];
             }
-        float score = s[0];
-#pragma unroll
-        for (int j = 1; j < N; ++j) score = at == (u32)j ? s[j] : score;
-        const u32 top = wave_max_u32(best);
-        const u32 from = (u32)__builtin_ctzll(ballot64(best == top));
-        const u32 e = (u32)__shfl((int)(lane * N + at), (int)from);
-        const float se = __shfl(score, (int)from);
-        if (lane == r) {
-            mine_e = e;
-            mine_s = se;
+            key[j] = e < P.experts ? KeyOf<RTOPK_F32>::key(__float_as_uint(c)) : 0u;
         }
+        if (P.groups > 1) {
+            wave_sync();  // (the last tokens' scores have been read)
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (lane == from && at == (u32)j) key[j] = 0;
+            for (int j = 0; j < N; ++j)
+                if (l * N + j < P.experts) ((u32*)mine)[S::place(l * N + j)] = key[j];
+            wave_sync();
+            // lane l takes groups l, l + L, ...: the keys of their two best
+            u32 group_key[64 / L];
+#pragma unroll
+            for (int t = 0; t < 64 / L; ++t) {
+                const u32 g = l + t * L;
+                u32 a = 0, b = 0;
+                if (g < P.groups)
+                    for (u32 i = 0; i < P.group_size; ++i) {
+                        const u32 v = ((const u32*)mine)[S::place(g * P.group_size + i)];
+                        b = max(b, min(a, v));
+                        a = max(a, v);
+                    }
+                group_key[t] = !top2 || b == 0 ? a : KeyOf<RTOPK_F32>::key(__float_as_uint(number_of_f32_key(a) + number_of_f32_key(b)));
+            }
+            wave_sync();
+#pragma unroll
+            for (int t = 0; t < 64 / L; ++t)
+                if (l + t * L < P.groups) ((u32*)mine)[l + t * L] = group_key[t];
+            wave_sync();
+            u32 better[64 / L] = {};
+            for (u32 g = 0; g < P.groups; ++g) {
+                const u32 o = ((const u32*)mine)[g];
+#pragma unroll
+                for (int t = 0; t < 64 / L; ++t) better[t] += o > group_key[t] || (o == group_key[t] && g < l + t * L);
+            }
+            u64 stays = 0;
+#pragma unroll
+            for (int t = 0; t < 64 / L; ++t) {
+                const u64 b = ballot64(l + t * L < P.groups && better[t] < P.topk_groups) >> (lane - l);
+                stays |= (L == 64 ? b : b & ((1ull << (L % 64)) - 1)) << (t * L % 64);
+            }
+            u32 g = l * N / P.group_size, left = (g + 1) * P.group_size - l * N;  // of the first of the lane's experts
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                if (left == 0) {
+                    ++g;
+                    left = P.group_size;
+                }
+                --left;
+                if (!((stays >> (g & 63)) & 1)) key[j] = 0;
+            }
+        }
+        wave_sync();
+#pragma unroll
+        for (int j = 0; j < N; ++j) mine[S::place(l * N + j)] = s[j];
+        for (u32 r = 0; r < P.k; ++r) {
+            u32 best = key[0];
+#pragma unroll
+            for (int j = 1; j < N; ++j) best = max(best, key[j]);
+            const u32 top = token_reduce<L>(best, UmaxOf{});
+            u64 from = ballot64(best == top) >> (lane - l);
+            if (L < 64) from &= (1ull << (L % 64)) - 1;
+            if (l == (u32)__builtin_ctzll(from)) {  // the token's lowest lane that has it, and the lowest of its experts
+                u32 at = 0;
+#pragma unroll
+                for (int j = N - 1; j >= 0; --j) at = key[j] == top ? (u32)j : at;
+#pragma unroll
+                for (int j = 0; j < N; ++j) key[j] = at == (u32)j ? 0u : key[j];
+                picked[r] = l * N + at;
+            }
+        }
+        wave_sync();
+        const u32 e = l < P.k ? picked[l] : 0;
+        const float se = mine[S::place(e)];
+        float w = se;
+        if (P.flags & RTOPK_ROUTE_RENORMALIZE) {
+            const float sum = token_reduce<L>(l < P.k ? se : 0.0f, AddOf{});
+            w = sum == 0.0f ? 0.0f : w / sum;
+        }
+        if (l < P.k && token < P.tokens) {
+            P.weights[row * P.k + l] = P.scale * w;
+            P.chosen[row * P.k + l] = (long long)e;
+            if (P.counts) atomicAdd(&tally[e], 1u);
+        }
     }
-    float w = mine_s;
-    if (P.flags & RTOPK_ROUTE_RENORMALIZE) {
-        const float sum = wave_sum(lane < P.k ? mine_s : 0.0f);
-        w = sum == 0.0f ? 0.0f : w / sum;
-    }
-    if (lane < P.k) {
-        P.weights[row * P.k + lane] = P.scale * w;
-        P.chosen[row * P.k + lane] = (long long)mine_e;
-        if (P.counts) atomicAdd(&P.counts[mine_e], 1ull);
+    if (P.counts) {
+        __syncthreads();
+        for (u32 i = threadIdx.x; i < P.experts; i += B)
+            if (tally[i]) atomicAdd(&P.counts[i], (unsigned long long)tally[i]);
     }
 }
 
 // softmax:  dx_j = s_j (G_j - sum_l G_l s_l), or, renormalised, over the chosen alone with their shares in the place of s
 // sigmoid:  dx_j = G_j s_j (1 - s_j), with G = (g - sum_l g_l share_l) / sum s where it is renormalised
-template <int DT, int N>
-__global__ void __launch_bounds__(kRouteBlock) k_route_grad(RouteParams P) {
-    __shared__ float stage[kRouteBlock / 64][64 * N];
-    const u32 lane = lane_id(), wave = threadIdx.x >> 6;
-    const long long row = P.row0 + (long long)blockIdx.x * (kRouteBlock / 64) + wave;
-    if (row >= P.tokens) return;
-    const char* x_row = P.logits + row * P.row_bytes;
-    char* out = P.grad + row * P.grad_bytes;
+constexpr int kRouteGradBlock = 256;
+
+template <int DT, int L, int N>
+__global__ void __launch_bounds__(kRouteGradBlock) k_route_grad(RouteParams P) {
+    typedef RouteShape<L, N> S;
+    __shared__ float stage[kRouteGradBlock / L][S::kStage];
+    const u32 lane = lane_id(), l = lane % L, slot = threadIdx.x / L;
     const bool sigmoid = (P.flags & RTOPK_ROUTE_SIGMOID) != 0, renormalize = (P.flags & RTOPK_ROUTE_RENORMALIZE) != 0;
-    float x[N], s[N];
+    constexpr u32 kWord = N * RowElem<DT>::kBytes < 16 ? N * RowElem<DT>::kBytes : 16;
+    const bool aligned = (((uintptr_t)P.logits | (uintptr_t)P.row_bytes) & (kWord - 1)) == 0, aligned_out = (((uintptr_t)P.grad | (uintptr_t)P.grad_bytes) & (kWord - 1)) == 0;
+    float* const mine = stage[slot];
+    for (long long first = (long long)blockIdx.x * (kRouteGradBlock / L); first < P.tokens; first += (long long)gridDim.x * (kRouteGradBlock / L)) {
+        const long long token = first + slot, row = token < P.tokens ? token : P.tokens - 1;
+        const long long e = l < P.k ? P.chosen[row * P.k + l] : -1;
+        const bool there = e >= 0 && e < (long long)P.experts;
+        float g = there ? P.scale * P.grad_weights[row * P.k + l] : 0.0f;
+        float x[N], s[N];
+        lane_logits<DT, N>(P.logits + row * P.row_bytes, l * N, P.experts, aligned, x);
+        scores_of<L, N>(x, s, sigmoid);
+        wave_sync();  // (the last tokens' sums have been read)
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const u32 e = lane * N + j;
-        x[j] = e < P.experts ? RowElem<DT>::load(x_row, e) : -__builtin_inff();
-    }
-    scores_of(x, s, sigmoid);
+        for (int j = 0; j < N; ++j) mine[S::place(l * N + j)] = s[j];
+        wave_sync();
+        const float se = there ? mine[S::place((u32)e)] : 0.0f;
+        if (renormalize) {
+            const float sum = token_reduce<L>(se, AddOf{}), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float mean = token_reduce<L>(g * se * inv, AddOf{});
+            g = (g - mean) * inv;
+        }
+        float dense = 0.0f;
+        if (!sigmoid && !renormalize) dense = token_reduce<L>(g * se, AddOf{});  // (renormalised, this sum is zero)
+        wave_sync();
 #pragma unroll
-    for (int j = 0; j < N; ++j) stage[wave][lane * N + j] = s[j];
-    wave_sync();
-    const long long e = lane < P.k ? P.chosen[row * P.k + lane] : -1;
-    const bool there = e >= 0 && e < (long long)P.experts;
-    const float se = there ? stage[wave][e] : 0.0f;
-    float g = there ? P.scale * P.grad_weights[row * P.k + lane] : 0.0f;
-    if (renormalize) {
-        const float sum = wave_sum(se), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const float mean = wave_sum(g * se * inv);
-        g = (g - mean) * inv;
-    }
-    float dense = 0.0f;
-    if (!sigmoid && !renormalize) dense = wave_sum(g * se);  // (renormalised, this sum is zero)
-    const float d = there ? g * (sigmoid ? se * (1.0f - se) : se) : 0.0f;
-    wave_sync();
+        for (int j = 0; j < N; ++j) mine[S::place(l * N + j)] = sigmoid ? 0.0f : -s[j] * dense;
+        wave_sync();
+        if (there) atomicAdd(&mine[S::place((u32)e)], g * (sigmoid ? se * (1.0f - se) : se));
+        wave_sync();
+        if (token < P.tokens) {
+            char* out = P.grad + row * P.grad_bytes;
+            constexpr int kBytes = N * RowElem<DT>::kBytes;
+            bool stored = false;
+            if constexpr (kBytes >= 4) {
+                if (aligned_out && l * N + N <= P.experts) {
+                    union { u32 w[kBytes / 4]; uint16_t h[kBytes / 2]; } q;
 #pragma unroll
-    for (int j = 0; j < N; ++j) stage[wave][lane * N + j] = sigmoid ? 0.0f : -s[j] * dense;
-    wave_sync();
-    if (there) atomicAdd(&stage[wave][e], d);
-    wave_sync();
+                    for (int j = 0; j < N; ++j) {
+                        const u32 b = RowElem<DT>::to_bits(mine[S::place(l * N + j)]);
+                        if constexpr (DT == RTOPK_F32) q.w[j] = b;
+                        else q.w[j / 2] = j & 1 ? q.w[j / 2] | (b << 16) : b;
+                    }
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const u32 i = lane * N + j;
-        if (i < P.experts) RowElem<DT>::store(out, i, stage[wave][i]);
+                    for (int i = 0; i < kBytes / (int)kWord; ++i) {
+                        char* p = out + (size_t)l * kBytes + i * kWord;
+                        if constexpr (kWord == 16) *(u32x4*)p = *(const u32x4*)&q.w[i * 4];
+                        else if constexpr (kWord == 8) *(uint2*)p = *(const uint2*)&q.w[0];
+                        else *(u32*)p = q.w[0];
+                    }
+                    stored = true;
+                }
+            }
+            if (!stored) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (l * N + j < P.experts) RowElem<DT>::store(out, l * N + j, mine[S::place(l * N + j)]);
+            }
+        }
     }
 }
 
@@ -217,14 +307,20 @@ static rtopk_status check_route(const void* logits, int64_t tokens, int64_t expe
     if (flags & ~(uint32_t)(RTOPK_ROUTE_SIGMOID | RTOPK_ROUTE_RENORMALIZE | RTOPK_ROUTE_GROUP_TOP2)) return RTOPK_ERR_INVALID_ARG;
     return RTOPK_OK;
 }
-// f(experts per lane)
+// f(lanes per token, experts per lane)
 template <class F>
-static rtopk_status by_experts(int64_t experts, F&& f) {
-    if (experts <= 64) return f(std::integral_constant<int, 1>{});
-    if (experts <= 128) return f(std::integral_constant<int, 2>{});
-    if (experts <= 256) return f(std::integral_constant<int, 4>{});
-    if (experts <= 512) return f(std::integral_constant<int, 8>{});
-    return f(std::integral_constant<int, 16>{});
+static rtopk_status by_experts(int64_t experts, int64_t k, F&& f) {
+    if (k <= 16) {
+        std::integral_constant<int, 16> lanes;
+        if (experts <= 16) return f(lanes, std::integral_constant<int, 1>{});
+        if (experts <= 64) return f(lanes, std::integral_constant<int, 4>{});
+        if (experts <= 128) return f(lanes, std::integral_constant<int, 8>{});
+        if (experts <= 256) return f(lanes, std::integral_constant<int, 16>{});
+    }
+    std::integral_constant<int, 64> lanes;
+    if (experts <= 256) return f(lanes, std::integral_constant<int, 4>{});
+    if (experts <= 512) return f(lanes, std::integral_constant<int, 8>{});
+    return f(lanes, std::integral_constant<int, 16>{});
 }
 
 }  // namespace rtopk
@@ -259,13 +355,16 @@ rtopk_status rtopk_route(const void* logits, int64_t tokens, int64_t experts, in
     P.counts = (unsigned long long*)counts;
     (void)hipGetLastError();  // an error left by earlier HIP calls of the process is not this call's
     return by_type(dt, [&](auto t) {
-        return by_experts(experts, [&](auto per_lane) {
-            constexpr int64_t kRows = kRouteBlock / 64;
-            for (; P.row0 < tokens; P.row0 += kMostWorkgroups * kRows) {
-                const int64_t wgs = (tokens - P.row0 + kRows - 1) / kRows;
-                hipLaunchKernelGGL((k_route<decltype(t)::value, decltype(per_lane)::value>), dim3((unsigned)(wgs < kMostWorkgroups ? wgs : kMostWorkgroups)), dim3(kRouteBlock),
-                                   0, (hipStream_t)hip_stream, P);
-            }
+        return by_experts(experts, k, [&](auto lanes, auto per_lane) {
+            constexpr int DT = decltype(t)::value, L = decltype(lanes)::value, N = decltype(per_lane)::value;
+            auto launch = [&](auto block, int64_t most) {
+                constexpr int B = decltype(block)::value;
+                const int64_t wgs = (tokens + B / L - 1) / (B / L);
+                hipLaunchKernelGGL((k_route<DT, L, N, B>), dim3((unsigned)(wgs < most ? wgs : most)), dim3(B), 0, (hipStream_t)hip_stream, P);
+            };
+            // Tokens are counted in LDS first.  Adds to one line of memory take 11 ns each, whoever makes them, so where they are counted few and large workgroups take all of them.
+            if (counts) launch(std::integral_constant<int, 1024>{}, 256);
+            else launch(std::integral_constant<int, 256>{}, 2048);
             return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
         });
     });
@@ -292,13 +391,10 @@ rtopk_status rtopk_route_backward(const void* logits, int64_t tokens, int64_t ex
     P.grad_bytes = grad_stride * (dt == RTOPK_F32 ? 4 : 2);
     (void)hipGetLastError();
     return by_type(dt, [&](auto t) {
-        return by_experts(experts, [&](auto per_lane) {
-            constexpr int64_t kRows = kRouteBlock / 64;
-            for (; P.row0 < tokens; P.row0 += kMostWorkgroups * kRows) {
-                const int64_t wgs = (tokens - P.row0 + kRows - 1) / kRows;
-                hipLaunchKernelGGL((k_route_grad<decltype(t)::value, decltype(per_lane)::value>), dim3((unsigned)(wgs < kMostWorkgroups ? wgs : kMostWorkgroups)),
-                                   dim3(kRouteBlock), 0, (hipStream_t)hip_stream, P);
-            }
+        return by_experts(experts, k, [&](auto lanes, auto per_lane) {
+            constexpr int DT = decltype(t)::value, L = decltype(lanes)::value, N = decltype(per_lane)::value;
+            const int64_t wgs = (tokens + kRouteGradBlock / L - 1) / (kRouteGradBlock / L);
+            hipLaunchKernelGGL((k_route_grad<DT, L, N>), dim3((unsigned)(wgs < 2048 ? wgs : 2048)), dim3(kRouteGradBlock), 0, (hipStream_t)hip_stream, P);
             return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
         });
     });

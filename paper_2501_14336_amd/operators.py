@@ -12,7 +12,6 @@ synchronises.
 """
 from __future__ import annotations
 
-import contextlib
 from typing import NamedTuple, Optional
 
 import torch
@@ -45,16 +44,20 @@ def _check(status):
 
 def _rows(x, what):
     """(address, batch, n, row stride, type) of a [batch, n] tensor whose rows are contiguous."""
+    shape = x.shape
     if not x.is_cuda:
         _refuse("%s must live on the GPU; there is no CPU path" % what)
-    if x.dim() != 2:
+    if len(shape) != 2:
         _refuse("%s must be a [batch, n] tensor" % what)
-    batch, n = x.shape
-    stride = x.stride(0) if batch > 1 else n
+    batch, n = shape
     if batch < 1 or n < 1:
         _refuse("%s is empty" % what)
-    if (n > 1 and x.stride(1) != 1) or stride < n:
-        _refuse("%s must have contiguous rows that do not overlap" % what)
+    stride = n
+    if not x.is_contiguous():
+        if batch > 1:
+            stride = x.stride(0)
+        if (n > 1 and x.stride(1) != 1) or stride < n:
+            _refuse("%s must have contiguous rows that do not overlap" % what)
     code = _CODES.get(x.dtype)
     if code is None:
         _refuse("%s must be float32, float16 or bfloat16" % what)
@@ -65,7 +68,7 @@ def _address(t, x, shape, dtype, what):
     """The address of a contiguous tensor beside the logits ``x``; None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or t.device != x.device or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != x.get_device() or not t.is_contiguous():
         _refuse("%s must be a contiguous %s tensor of shape %s on %s" % (what, dtype, tuple(shape), x.device))
     return t.data_ptr()
 
@@ -77,16 +80,20 @@ def _inverse(temperature):
     return 1.0 / temperature
 
 
-_here = contextlib.nullcontext()
+# (a stream's handle without the object around it: 0.1 us instead of 2, where a call's own work takes 5)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _on(x):
-    """The device that ``x`` lives on, made current if it is not."""
-    return _here if x.device.index == torch.cuda.current_device() else torch.cuda.device(x.device)
-
-
-def _stream(x):
-    return torch.cuda.current_stream(x.device).cuda_stream
+def _enqueue(x, call, *args):
+    """The C call with the stream that is current on x's device, which is made current if it is not."""
+    device = x.get_device()
+    if device == torch.cuda.current_device():
+        status = call(*args, _raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = call(*args, _raw_stream(device))
+    if status != _B.RTOPK_OK:
+        raise RtopkError(status, _B.rtopk_status_string(status))
 
 
 def _tokens_2d(tokens):
@@ -140,10 +147,8 @@ def _logprobs(logits, tokens, k, inv_temperature, entropy, workspace):
     top, at = (new((batch, k)), new((batch, k), torch.int64)) if k else (None, None)
     need = _size(lib, "rtopk_logprobs_workspace_bytes", batch, n, m, k, code)
     ws = _workspace(workspace, need, logits)
-    with _on(logits):
-        _check(lib.rtopk_logprobs(x, batch, n, stride, code, inv_temperature, t, m, k, lp.data_ptr(), h.data_ptr() if entropy else None,
-                                  stats.data_ptr(), top.data_ptr() if k else None, at.data_ptr() if k else None, ws.data_ptr(),
-                                  ws.numel() * ws.element_size(), _stream(logits)))
+    _enqueue(logits, lib.rtopk_logprobs, x, batch, n, stride, code, inv_temperature, t, m, k, lp.data_ptr(), h.data_ptr() if entropy else None,
+             stats.data_ptr(), top.data_ptr() if k else None, at.data_ptr() if k else None, ws.data_ptr(), ws.numel() * ws.element_size())
     return LogProbs(lp, top, at, h, stats)
 
 
@@ -199,8 +204,7 @@ def logprobs_backward(logits, tokens, row_stats, grad_logprobs, entropy=None, gr
             _address(row_stats, logits, (batch, 2), f32, "row_stats"),
             _address(grad_logprobs, logits, (batch, m), f32, "grad_logprobs") if m else None,
             _address(entropy, logits, (batch,), f32, "entropy"), _address(grad_entropy, logits, (batch,), f32, "grad_entropy"))
-    with _on(logits):
-        _check(lib.rtopk_logprobs_backward(x, batch, n, stride, code, _inverse(temperature), *args, g, g_stride, _stream(logits)))
+    _enqueue(logits, lib.rtopk_logprobs_backward, x, batch, n, stride, code, _inverse(temperature), *args, g, g_stride)
     return out
 
 
@@ -229,8 +233,7 @@ def _distill(student, values, indices, teacher_lse, temperature, workspace):
     loss = torch.empty((batch,), dtype=torch.float32, device=student.device)
     stats = torch.empty((batch, DISTILL_ROW_STATS), dtype=torch.float32, device=student.device)
     ws = _workspace(workspace, _size(lib, "rtopk_distill_workspace_bytes", batch, n, k, code), student)
-    with _on(student):
-        _check(lib.rtopk_distill(*args, loss.data_ptr(), stats.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(student)))
+    _enqueue(student, lib.rtopk_distill, *args, loss.data_ptr(), stats.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size())
     return loss, stats
 
 
@@ -274,8 +277,7 @@ def distill_backward(student, teacher_values, teacher_indices, row_stats, grad_l
     g, _, _, g_stride, _ = _rows(out, "out")
     stats = _address(row_stats, student, (args[1], DISTILL_ROW_STATS), torch.float32, "row_stats")
     w = _address(grad_loss, student, (args[1],), torch.float32, "grad_loss")
-    with _on(student):
-        _check(lib.rtopk_distill_backward(*args, stats, w, g, g_stride, _stream(student)))
+    _enqueue(student, lib.rtopk_distill_backward, *args, stats, w, g, g_stride)
     return out
 
 
@@ -290,8 +292,7 @@ def distill_step(student, teacher_values, teacher_indices, row_weights, teacher_
     g, _, _, g_stride, _ = _rows(out, "out")
     w = _address(row_weights, student, (batch,), torch.float32, "row_weights")
     ws = _workspace(workspace, _size(lib, "rtopk_distill_workspace_bytes", batch, n, k, code), student)
-    with _on(student):
-        _check(lib.rtopk_distill_step(*args, w, loss.data_ptr(), g, g_stride, ws.data_ptr(), ws.numel() * ws.element_size(), _stream(student)))
+    _enqueue(student, lib.rtopk_distill_step, *args, w, loss.data_ptr(), g, g_stride, ws.data_ptr(), ws.numel() * ws.element_size())
     return loss, out
 
 
@@ -312,9 +313,8 @@ def _route(logits, k, flags, bias, groups, topk_groups, scale, counts):
     chosen = torch.empty((tokens, max(k, 0)), dtype=torch.int64, device=logits.device)
     b = _address(bias, logits, (experts,), torch.float32, "bias")
     c = _address(counts, logits, (experts,), torch.int64, "counts")
-    with _on(logits):
-        _check(lib.rtopk_route(x, tokens, experts, stride, code, b, groups, topk_groups, k, flags, scale, weights.data_ptr(), chosen.data_ptr(), c,
-                               _stream(logits)))
+    _enqueue(logits, lib.rtopk_route, x, tokens, experts, stride, code, b, groups, topk_groups, k, flags, scale, weights.data_ptr(),
+             chosen.data_ptr(), c)
     return weights, chosen
 
 
@@ -360,8 +360,7 @@ def _route_backward(logits, experts, grad_weights, flags, scale, out):
     g, _, _, g_stride, _ = _rows(out, "out")
     e = _address(experts, logits, (tokens, k), torch.int64, "experts")
     w = _address(grad_weights, logits, (tokens, k), torch.float32, "grad_weights")
-    with _on(logits):
-        _check(lib.rtopk_route_backward(x, tokens, n, stride, code, e, k, flags, scale, w, g, g_stride, _stream(logits)))
+    _enqueue(logits, lib.rtopk_route_backward, x, tokens, n, stride, code, e, k, flags, scale, w, g, g_stride)
     return out
 
 
