@@ -29,7 +29,7 @@ struct RouteParams {
 template <int L, int N>
 struct RouteShape {
     static constexpr int kTokens = 64 / L;                    // of a wave
-    static constexpr int kStage = L * N + L * N / 32 + L;     // words of LDS per token: its row with a word after every 32 (groups of 32 and 64 begin in different banks), and what was chosen
+    static constexpr int kStage = L * N + L * N / 32;         // words of LDS per token: its row with a word after every 32 (groups of 32 and 64 begin in different banks)
     static constexpr u32 place(u32 e) { return e + e / 32; }  // of an expert's word
 };
 
@@ -55,7 +55,6 @@ __device__ __forceinline__ T token_reduce(T v, Op&& op) {
 }
 struct AddOf { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 struct FmaxOf { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
-struct UmaxOf { __device__ __forceinline__ u32 operator()(u32 a, u32 b) const { return max(a, b); } };
 
 // What the wave's lanes wrote to LDS is there for all of them.
 __device__ __forceinline__ void wave_sync() {
@@ -109,68 +108,139 @@ __device__ __forceinline__ void scores_of(const float (&x)[N], float (&s)[N], bo
     for (int j = 0; j < N; ++j) s[j] = sum == 0.0f ? 0.0f : s[j] / sum;
 }
 
+// A choice: its key above the complement of its expert, 42 bits, so that all are different and the larger is the better one.  The same bits read as a 64-bit float are one of the numbers
+// next to zero, which order as the bits do; minimum and maximum of them are one instruction each where a 64-bit comparison and its selects are five.  (Written out: the compiler
+// would first make sure that neither is a NaN.)
+constexpr u32 kExpertBits = 10;
+static_assert(RTOPK_ROUTE_MAX_EXPERTS <= 1 << kExpertBits, "an expert's number has its bits");
+__device__ __forceinline__ double choice_of(u32 key, u32 e) { return __builtin_bit_cast(double, ((u64)key << kExpertBits) | ((1u << kExpertBits) - 1u - e)); }
+__device__ __forceinline__ u32 expert_of(double c) { return (1u << kExpertBits) - 1u - ((u32)__builtin_bit_cast(u64, c) & ((1u << kExpertBits) - 1u)); }
+__device__ __forceinline__ double larger(double a, double b) {
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ double smaller(double a, double b) {
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+
+// Best first (odd-even merge sort).
+template <int N>
+__device__ __forceinline__ void sort_choices(double (&c)[N]) {
+#pragma unroll
+    for (int p = 1; p < N; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int j = k % p; j + k < N; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const double a = c[i + j], b = c[i + j + k];
+                        c[i + j] = larger(a, b);
+                        c[i + j + k] = smaller(a, b);
+                    }
+}
+
+template <int CTRL>
+__device__ __forceinline__ u32 lane_swapped(u32 v) { return (u32)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false); }
+// The two best keys of two sets.
+__device__ __forceinline__ void best_two(u32& a, u32& b, u32 a2, u32 b2) {
+    b = max(min(a, a2), max(b, b2));
+    a = max(a, a2);
+}
+
 template <int DT, int L, int N, int B>
 __global__ void __launch_bounds__(B) k_route(RouteParams P) {
     typedef RouteShape<L, N> S;
     __shared__ float stage[B / L][S::kStage];
     __shared__ u32 tally[L * N];  // what this workgroup's tokens chose
-    const u32 lane = lane_id(), wave = threadIdx.x >> 6, l = lane % L, slot = threadIdx.x / L;
+    const u32 lane = lane_id(), slot = threadIdx.x / L;
     const bool sigmoid = (P.flags & RTOPK_ROUTE_SIGMOID) != 0, top2 = (P.flags & RTOPK_ROUTE_GROUP_TOP2) != 0;
-    constexpr u32 kWord = N * RowElem<DT>::kBytes < 16 ? N * RowElem<DT>::kBytes : 16;
+    constexpr u32 kWord = N * RowElem<DT>::kBytes < 16 ? N * RowElem<DT>::kBytes : 16, kBiasWord = N * 4 < 16 ? N * 4 : 16;
     const bool aligned = (((uintptr_t)P.logits | (uintptr_t)P.row_bytes) & (kWord - 1)) == 0;
+    // groups of whole lanes, as many as a power of two: their best two are found on the way across those lanes
+    const u32 group_lanes = P.group_size / N;
+    const bool by_lanes = group_lanes * N == P.group_size && (group_lanes & (group_lanes - 1)) == 0 && group_lanes <= 16;
     if (P.counts) {
         for (u32 i = threadIdx.x; i < P.experts; i += B) tally[i] = 0;
         __syncthreads();
     }
     float* const mine = stage[slot];
-    u32* const picked = (u32*)(mine + L * N + L * N / 32);
     for (long long first = (long long)blockIdx.x * (B / L); first < P.tokens; first += (long long)gridDim.x * (B / L)) {
         // (lanes of a token that is none work on the last one's row, and store nothing)
         const long long token = first + slot, row = token < P.tokens ? token : P.tokens - 1;
-        float x[N], s[N];
+        u32 l = lane % L;
+        asm volatile("" : "+v"(l));  // (what depends on the lane alone is made anew for every token: kept, it takes more registers than there are)
+        float x[N], s[N], bias[N];
         lane_logits<DT, N>(P.logits + row * P.row_bytes, l * N, P.experts, aligned, x);
+        if (P.bias) lane_logits<RTOPK_F32, N>((const char*)P.bias, l * N, P.experts, ((uintptr_t)P.bias & (kBiasWord - 1)) == 0, bias);
         scores_of<L, N>(x, s, sigmoid);
         u32 key[N];  // orders the choice; 0 for what may not be chosen
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const u32 e = l * N + j;
-            float c = x[j];
-            if (x[j] != -__builtin_inff()) {
-                if (P.bias) c = s[j] + (e < P.experts ? P.bias[e] : 0.0f);
-                else if (top2) c = s[j];
-            }
-            key[j] = e < P.experts ? KeyOf<RTOPK_F32>::key(__float_as_uint(c)) : 0u;
+            float c = P.bias ? s[j] + bias[j] : top2 ? s[j] : x[j];
+            c = x[j] == -__builtin_inff() ? x[j] : c;
+            key[j] = KeyOf<RTOPK_F32>::key(__float_as_uint(c));
         }
-        if (P.groups > 1) {
-            wave_sync();  // (the last tokens' scores have been read)
+        if (l * N + N > P.experts) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) key[j] = l * N + j < P.experts ? key[j] : 0u;
+        }
+        wave_sync();  // (the last tokens' scores have been read)
+        auto group_value = [&](u32 a, u32 b) { return !top2 || b == 0 ? a : KeyOf<RTOPK_F32>::key(__float_as_uint(number_of_f32_key(a) + number_of_f32_key(b))); };
+        if (P.groups > 1 && by_lanes) {
+            u32 a = key[0], b = 0;
+#pragma unroll
+            for (int j = 1; j < N; ++j) {
+                b = max(b, min(a, key[j]));
+                a = max(a, key[j]);
+            }
+            if (group_lanes >= 2) best_two(a, b, lane_swapped<0xb1>(a), lane_swapped<0xb1>(b));      // 1 apart
+            if (group_lanes >= 4) best_two(a, b, lane_swapped<0x4e>(a), lane_swapped<0x4e>(b));      // 2
+            if (group_lanes >= 8) best_two(a, b, lane_swapped<0x141>(a), lane_swapped<0x141>(b));    // the other four of eight
+            if (group_lanes >= 16) best_two(a, b, lane_swapped<0x140>(a), lane_swapped<0x140>(b));   // the other eight of sixteen
+            const u32 value = group_value(a, b), group = l / group_lanes;
+            if (group < P.groups) ((u32*)mine)[group] = value;
+            wave_sync();
+            u32 better = 0;
+#pragma clang loop unroll(disable)
+            for (u32 g = 0; g < P.groups; ++g) {
+                const u32 o = ((const u32*)mine)[g];
+                better += o > value || (o == value && g < group);
+            }
+            if (better >= P.topk_groups) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) key[j] = 0;
+            }
+        } else if (P.groups > 1) {
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 if (l * N + j < P.experts) ((u32*)mine)[S::place(l * N + j)] = key[j];
             wave_sync();
-            // lane l takes groups l, l + L, ...: the keys of their two best
-            u32 group_key[64 / L];
+            // lane l takes groups l, l + L, ...
+            u32 value[64 / L];
 #pragma unroll
             for (int t = 0; t < 64 / L; ++t) {
-                const u32 g = l + t * L;
                 u32 a = 0, b = 0;
-                if (g < P.groups)
-                    for (u32 i = 0; i < P.group_size; ++i) {
-                        const u32 v = ((const u32*)mine)[S::place(g * P.group_size + i)];
-                        b = max(b, min(a, v));
-                        a = max(a, v);
-                    }
-                group_key[t] = !top2 || b == 0 ? a : KeyOf<RTOPK_F32>::key(__float_as_uint(number_of_f32_key(a) + number_of_f32_key(b)));
+                if (l + t * L < P.groups)
+#pragma clang loop unroll(disable)
+                    for (u32 i = 0; i < P.group_size; ++i) best_two(a, b, ((const u32*)mine)[S::place((l + t * L) * P.group_size + i)], 0);
+                value[t] = group_value(a, b);
             }
             wave_sync();
 #pragma unroll
             for (int t = 0; t < 64 / L; ++t)
-                if (l + t * L < P.groups) ((u32*)mine)[l + t * L] = group_key[t];
+                if (l + t * L < P.groups) ((u32*)mine)[l + t * L] = value[t];
             wave_sync();
             u32 better[64 / L] = {};
+#pragma clang loop unroll(disable)
             for (u32 g = 0; g < P.groups; ++g) {
                 const u32 o = ((const u32*)mine)[g];
 #pragma unroll
-                for (int t = 0; t < 64 / L; ++t) better[t] += o > group_key[t] || (o == group_key[t] && g < l + t * L);
+                for (int t = 0; t < 64 / L; ++t) better[t] += o > value[t] || (o == value[t] && g < l + t * L);
             }
             u64 stays = 0;
 #pragma unroll
@@ -192,24 +262,35 @@ __global__ void __launch_bounds__(B) k_route(RouteParams P) {
         wave_sync();
 #pragma unroll
         for (int j = 0; j < N; ++j) mine[S::place(l * N + j)] = s[j];
+        // every lane's choices in order; the best of the lanes' first is taken k times
+        double c[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) c[j] = choice_of(key[j], l * N + j);
+        sort_choices(c);
+        u32 e = 0;
+#pragma clang loop unroll(disable)
         for (u32 r = 0; r < P.k; ++r) {
-            u32 best = key[0];
+            double top = c[0];
+            auto across = [&](auto ctrl) {
+                const u64 v = __builtin_bit_cast(u64, top);
+                top = larger(top, __builtin_bit_cast(double, ((u64)row_rotated<decltype(ctrl)::value>((u32)(v >> 32)) << 32) | row_rotated<decltype(ctrl)::value>((u32)v)));
+            };
+            across(std::integral_constant<int, 0x128>{});
+            across(std::integral_constant<int, 0x124>{});
+            across(std::integral_constant<int, 0x122>{});
+            across(std::integral_constant<int, 0x121>{});
+            if constexpr (L == 64) {
+                top = larger(top, __shfl_xor(top, 16));
+                top = larger(top, __shfl_xor(top, 32));
+            }
+            if (l == r) e = expert_of(top);
+            if (__builtin_bit_cast(u64, c[0]) == __builtin_bit_cast(u64, top)) {
 #pragma unroll
-            for (int j = 1; j < N; ++j) best = max(best, key[j]);
-            const u32 top = token_reduce<L>(best, UmaxOf{});
-            u64 from = ballot64(best == top) >> (lane - l);
-            if (L < 64) from &= (1ull << (L % 64)) - 1;
-            if (l == (u32)__builtin_ctzll(from)) {  // the token's lowest lane that has it, and the lowest of its experts
-                u32 at = 0;
-#pragma unroll
-                for (int j = N - 1; j >= 0; --j) at = key[j] == top ? (u32)j : at;
-#pragma unroll
-                for (int j = 0; j < N; ++j) key[j] = at == (u32)j ? 0u : key[j];
-                picked[r] = l * N + at;
+                for (int j = 0; j + 1 < N; ++j) c[j] = c[j + 1];
+                c[N - 1] = 0.0;
             }
         }
         wave_sync();
-        const u32 e = l < P.k ? picked[l] : 0;
         const float se = mine[S::place(e)];
         float w = se;
         if (P.flags & RTOPK_ROUTE_RENORMALIZE) {
