@@ -71,15 +71,15 @@ __global__ void __launch_bounds__(kDistillBlock) k_distill_part(DistillParams P)
         float x[kDistillVecs * E];
 #pragma unroll
         for (int i = 0; i < kDistillVecs; ++i) {
-            float y[E];
-            RowElem<DT>::unpack(q[i], y);
-            u32 out = 0;
+            u32 bits = 0;
             if (TAIL) {
                 const u32 v = first + i * kDistillBlock + threadIdx.x;
-                if (v < v1) out = ((const uint8_t*)marks)[v - v0];
+                if (v < v1) bits = ((const uint8_t*)marks)[v - v0];
             }
+            float y[E];
+            RowElem<DT>::unpack(TAIL ? RowElem<DT>::without(q[i], bits) : q[i], y);
 #pragma unroll
-            for (int j = 0; j < E; ++j) x[i * E + j] = TAIL && ((out >> j) & 1) ? -__builtin_inff() : y[j];
+            for (int j = 0; j < E; ++j) x[i * E + j] = y[j];
         }
         soft_add<false>(a, x, P.c);
     });
@@ -95,6 +95,35 @@ __global__ void __launch_bounds__(kDistillBlock) k_distill_part(DistillParams P)
 // ln of an entry's share.
 __device__ __forceinline__ float ln_share(float z, const DistillRow& d, bool tail, float ln_zmul, float inv_t) {
     return tail ? z * inv_t - d.zref : (z - d.zref) * inv_t + ln_zmul;
+}
+
+// A row's statistics from the sums of all its columns (a), of those that are not listed (others), of the teacher's list (zs), and of its shares (share): fills d, whose zref and zmul
+// are there, and returns the rest's part of the loss.
+template <bool TAIL>
+__device__ __forceinline__ float finish_row(DistillRow& d, const SoftSum& a, const SoftSum& others, double share, float zs, const DistillParams& P) {
+    d.m = a.m;
+    d.s = a.s;
+    d.spare = 0.0f;
+    if (!TAIL) {
+        d.q = zs == 0.0f ? 0.0f : zs != zs ? zs : 1.0f;
+        d.mu = finite_or_zero(a.m);
+        d.dense = a.s == 0.0f ? 0.0f : d.q / a.s;
+        return 0.0f;
+    }
+    const float rest = share < 1.0 ? (float)(1.0 - share) : share != share ? (float)share : 0.0f;
+    const float ln_other = others.s == 0.0f ? -__builtin_inff() : (others.m - a.m) * P.inv_t + kLn2 * (log2_fast(others.s) - log2_fast(a.s));
+    d.q = share < 1.0 ? 1.0f : (float)share;
+    d.mu = finite_or_zero(others.m);
+    d.dense = others.s == 0.0f ? 0.0f : d.q * exp2_fast((d.mu - finite_or_zero(a.m)) * P.c) / a.s - rest / others.s;
+    return rest != 0.0f ? rest * (kLn2 * log2_fast(rest) - ln_other) : 0.0f;
+}
+
+// An entry's share under the teacher's log-sum, without the rounding of its logarithm: what all of them leave of 1 may be a millionth.
+__device__ __forceinline__ double exact_share(float z, float lse, float inv_t) {
+    const float p = z * inv_t, low = __builtin_fmaf(z, inv_t, -p), hi = p - lse, back = hi - p;  // p + low is z inv_t exactly; hi + rest is p - lse exactly
+    const float rest = (p - (hi - back)) + (-lse - back);
+    const double e = (double)expf(hi);
+    return fabsf(hi) < 1e30f ? e * (1.0 + (double)(low + rest)) : e;  // (a masked entry has none to add)
 }
 
 constexpr int kDistillFinish = 256;
@@ -116,9 +145,6 @@ __global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams
     const SoftSum others = a;
     if (tail) a = soft_join<false>(a, soft_block<kDistillFinish, false>(listed, P.c, sm[1]), P.c);
     DistillRow d;
-    d.m = a.m;
-    d.s = a.s;
-    d.spare = 0.0f;
     float ln_zmul = 0.0f;
     if (tail) {
         d.zref = P.teacher_lse[row];
@@ -136,12 +162,12 @@ __global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams
     }
     const float ln_s = kLn2 * log2_fast(a.s);
     float loss = 0.0f;
-    double q = 0.0;  // (what is left of 1 may be a millionth: its logarithm counts)
+    double q = 0.0;
     for (long long i = threadIdx.x; i < P.k; i += kDistillFinish) {
         const long long t = columns[i];
         if (t < 0) continue;
         const float z = load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i)), lq = ln_share(z, d, tail, ln_zmul, P.inv_t), qi = expf(lq);
-        if (tail) q += exp((double)z * (double)P.inv_t - (double)d.zref);
+        if (tail) q += exact_share(z, d.zref, P.inv_t);
         if (t >= (long long)P.n) {
             loss += __builtin_nanf("");
         } else if (qi != 0.0f) {
@@ -150,19 +176,8 @@ __global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams
         }
     }
     loss = sum_block<kDistillFinish>(loss, (float*)sums[0]);
-    if (tail) {
-        q = sum_block<kDistillFinish>(q, sums[1]);
-        const float rest = q < 1.0 ? (float)(1.0 - q) : q != q ? (float)q : 0.0f;
-        const float ln_other = others.s == 0.0f ? -__builtin_inff() : (others.m - a.m) * P.inv_t + kLn2 * log2_fast(others.s) - ln_s;
-        if (rest != 0.0f) loss += rest * (kLn2 * log2_fast(rest) - ln_other);
-        d.q = q < 1.0 ? 1.0f : (float)q;
-        d.mu = finite_or_zero(others.m);
-        d.dense = others.s == 0.0f ? 0.0f : d.q * exp2_fast((d.mu - finite_or_zero(a.m)) * P.c) / a.s - rest / others.s;
-    } else {
-        d.q = z.s == 0.0f ? 0.0f : z.s != z.s ? z.s : 1.0f;
-        d.mu = finite_or_zero(a.m);
-        d.dense = a.s == 0.0f ? 0.0f : d.q / a.s;
-    }
+    if (tail) q = sum_block<kDistillFinish>(q, sums[1]);
+    loss += tail ? finish_row<true>(d, a, others, q, z.s, P) : finish_row<false>(d, a, others, q, z.s, P);
     if (threadIdx.x == 0) {
         P.loss[row] = loss;
         if (P.rows) P.rows[row] = d;
@@ -173,7 +188,7 @@ constexpr int kDistillGradBlock = 256, kDistillGradVecs = 4;
 
 template <int DT>
 __global__ void __launch_bounds__(kDistillGradBlock) k_distill_grad(DistillParams P) {
-    extern __shared__ u32 marks[];
+    extern __shared__ __align__(16) u32 lds[];
     __shared__ u32 twice;
     const u32 part = blockIdx.x % P.parts;
     const long long row = P.row0 + blockIdx.x / P.parts;
@@ -185,20 +200,226 @@ __global__ void __launch_bounds__(kDistillGradBlock) k_distill_grad(DistillParam
     const DistillRow d = P.rows[row];
     const float g = P.grad_loss[row] * P.inv_t, a = g * d.dense, b = d.s == 0.0f ? 0.0f : d.q / d.s, m = finite_or_zero(d.m);
     const bool tail = P.teacher_lse != nullptr;
-    write_gradient<DT, kDistillGradBlock, kDistillGradVecs, false>(
-        r, out, aligned, v0, v1, g == 0.0f ? 0 : P.k, marks, &twice, [&](long long i) { return columns[i]; },
+    if (g == 0.0f) {  // (padding: its logits may be anything)
+        for (u32 v = v0 + threadIdx.x; v < v1; v += kDistillGradBlock) {
+            const float none[RowElem<DT>::E] = {};
+            store_vector<DT>(r, out, aligned, v, none);
+        }
+        return;
+    }
+    write_gradient<DT, kDistillGradBlock, kDistillGradVecs, 4, false>(
+        r, out, aligned, v0, v1, P.k, lds, &twice, [&](long long i) { return columns[i]; },
         [&](long long i) {
             const float z = load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i));
             return expf(ln_share(z, d, tail, 0.0f, P.inv_t)) * d.zmul;
         },
-        [&](float x) { return g == 0.0f ? 0.0f : a * exp2_fast((x - d.mu) * P.c); },
+        [&](float x) { return a * exp2_fast((x - d.mu) * P.c); },
         [&](float x, float q) { return g * (b * exp2_fast((x - m) * P.c) - q); });
+}
+
+// Loss and gradient in one launch: a workgroup holds its row in registers between the two, so that the row is read once, and written once.
+template <int DT, int B, int NV, bool TAIL>
+__global__ void __launch_bounds__(B, 4) k_distill_step(DistillParams P) {
+    extern __shared__ __align__(16) u32 lds[];
+    __shared__ u32 twice;
+    __shared__ float4 sm[3][B / 64];
+    __shared__ double sums[2][B / 64];
+    constexpr int E = RowElem<DT>::E, R = B >= 1024 ? 1 : B >= 512 ? 2 : 4, kChunk = 2;
+    const long long row = P.row0 + blockIdx.x;
+    const RowView<DT> r(P.student, row, P.row_bytes, P.n);
+    char* out = P.grad + row * P.grad_bytes;
+    const bool aligned = (((uintptr_t)out ^ (uintptr_t)r.x) & 15) == 0;
+    const long long* columns = P.columns + row * P.k;
+    const float g = P.grad_loss[row] * P.inv_t;
+    // the thread's entries first, then its part of the row: it is on its way while the teacher's side is done
+    long long col[R];
+    float z[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const long long i = threadIdx.x + (long long)k * B;
+        col[k] = i < P.k ? columns[i] : -1;
+        z[k] = i < P.k ? load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i)) : 0.0f;
+    }
+    u32x4 q[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const u32 v = i * B + threadIdx.x;
+        if ((u32)(i + 1) * B <= r.nvec && r.whole(i * B) && r.whole(i * B + B - 1)) {
+            q[i] = r.template load<true>(v);
+        } else {
+            q[i] = u32x4{RowElem<DT>::kMinusInf, RowElem<DT>::kMinusInf, RowElem<DT>::kMinusInf, RowElem<DT>::kMinusInf};
+            if (v < r.nvec) q[i] = r.trimmed(r.template load<true>(v), v);
+        }
+    }
+    float x_of[R];  // the entries' logits
+#pragma unroll
+    for (int k = 0; k < R; ++k) x_of[k] = col[k] >= 0 && col[k] < (long long)P.n ? RowElem<DT>::load(r.x, (u32)col[k]) : 0.0f;
+    DistillRow d;
+    d.zref = TAIL ? P.teacher_lse[row] : 0.0f;
+    float ln_zmul = 0.0f, zs = 1.0f;
+    if (!TAIL) {
+        SoftSum a;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const float v[1] = {col[k] >= 0 ? z[k] : -__builtin_inff()};
+            soft_add<false>(a, v, P.c);
+        }
+        for (long long i = threadIdx.x + (long long)R * B; i < P.k; i += B)
+            if (columns[i] >= 0) {
+                const float v[1] = {load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i))};
+                soft_add<false>(a, v, P.c);
+            }
+        a = soft_block<B, false>(a, P.c, sm[0]);
+        d.zref = finite_or_zero(a.m);
+        zs = a.s;
+        ln_zmul = zs == 0.0f ? 0.0f : -kLn2 * log2_fast(zs);
+    }
+    auto ln_q = [&](float v) { return ln_share(v, d, TAIL, ln_zmul, P.inv_t); };
+    float loss = 0.0f;
+    double share = 0.0;  // TAIL: of all that is listed
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        if (col[k] >= (long long)P.n) loss = __builtin_nanf("");
+        if (TAIL && col[k] >= 0) share += exact_share(z[k], d.zref, P.inv_t);
+        z[k] = ln_q(z[k]);
+    }
+    for (long long i = threadIdx.x + (long long)R * B; i < P.k; i += B) {
+        const long long t = columns[i];
+        if (t >= (long long)P.n) loss = __builtin_nanf("");
+        if (TAIL && t >= 0) share += exact_share(load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i)), d.zref, P.inv_t);
+    }
+    SoftSum listed;
+    const auto at = [&](long long i) { return columns[i]; };
+    const auto ln_value = [&](long long i) { return ln_q(load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i))); };
+    const auto value = [&](long long i) { return expf(ln_value(i)); };
+    ListedColumns<DT, B, 1, R, decltype(at), decltype(value)> list(
+        r, 0, r.nvec, P.k, lds, &twice, at, value,
+        [&](int k, long long& t, float& v) {
+            t = col[k];
+            v = expf(z[k]);
+        },
+        [&](u32 p) {
+            if (TAIL) {
+                const float x[1] = {RowElem<DT>::load(r.x, p - r.lead)};
+                soft_add<false>(listed, x, P.c);
+            }
+        });
+    // first pass: the softmax; TAIL: of what is not listed
+    SoftSum a;
+#pragma unroll
+    for (int i0 = 0; i0 < NV; i0 += kChunk) {
+        float x[kChunk * E];
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            const u32 v = (i0 + i) * B + threadIdx.x;
+            float y[E];
+            // (without a branch: with one, the compiler keeps both sides' registers)
+            RowElem<DT>::unpack(TAIL ? RowElem<DT>::without(q[i0 + i], list.any && v < r.nvec ? list.listed_of(v) : 0) : q[i0 + i], y);
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[i * E + j] = y[j];
+        }
+        soft_add<false>(a, x, P.c);
+        asm volatile("" ::: "memory");  // (a chunk at a time: registers)
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // (the second pass converts the row anew: kept as 32-bit numbers, it would not fit)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(q[i]));
+    if (TAIL) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const float x[1] = {list.any && list.fresh[k] ? x_of[k] : -__builtin_inff()};
+            soft_add<false>(listed, x, P.c);
+        }
+    }
+    a = soft_block<B, false>(a, P.c, sm[1]);
+    const SoftSum others = a;
+    if (TAIL) a = soft_join<false>(a, soft_block<B, false>(listed, P.c, sm[2]), P.c);
+    if (TAIL) share = sum_block<B>(share, sums[0]);
+    const float of_rest = finish_row<TAIL>(d, a, others, share, zs, P);
+    if (threadIdx.x == 0) loss += of_rest;
+    // the entries: their part of the loss, and their columns' gradients
+    const float scale = g * d.dense, b = d.s == 0.0f ? 0.0f : d.q / d.s, m = finite_or_zero(d.m), ln_s = kLn2 * log2_fast(d.s);
+    auto loss_of = [&](float lq, float x) {
+        const float qi = expf(lq);
+        return qi != 0.0f ? qi * (lq - (d.s == 0.0f ? -__builtin_inff() : (x - d.m) * P.inv_t - ln_s)) : 0.0f;
+    };
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+        if (col[k] >= 0 && col[k] < (long long)P.n) loss += loss_of(z[k], x_of[k]);
+    for (long long i = threadIdx.x + (long long)R * B; i < P.k; i += B) {
+        const long long t = columns[i];
+        if (t >= 0 && t < (long long)P.n) loss += loss_of(ln_value(i), RowElem<DT>::load(r.x, (u32)t));
+    }
+    auto of_column = [&](int k, u32 p, float sum) {
+        float x = 0.0f;
+        if (k < 0) x = RowElem<DT>::load(r.x, p - r.lead);
+#pragma unroll
+        for (int l = 0; l < R; ++l) x = k == l ? x_of[l] : x;
+        return g * (b * exp2_fast((x - m) * P.c) - sum);
+    };
+    list.work_out(of_column);
+    // second pass: the gradient
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const u32 v = i * B + threadIdx.x;
+        if (list.any && (u32)i * B < r.nvec) {
+            list.put(i * B * E, of_column);
+            __syncthreads();
+        }
+        if (v < r.nvec) {
+            float x[E];
+            RowElem<DT>::unpack(q[i], x);
+            gradient_of_vector<DT>(x, list.any ? list.listed_of(v) : 0, list.tile + threadIdx.x * E, [&](float y) { return scale * exp2_fast((y - d.mu) * P.c); });
+            if (g == 0.0f) {  // (padding: its logits may be anything)
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] = 0.0f;
+            }
+            store_vector<DT>(r, out, aligned, v, x);
+        }
+        if (list.any && (u32)i * B < r.nvec) __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    loss = sum_block<B>(loss, (float*)sums[1]);
+    if (threadIdx.x == 0) P.loss[row] = loss;
 }
 
 constexpr int64_t kDistillMostVecs = (int64_t)1 << 15;  // (the bitmaps: a byte each)
 
 static RowParts distill_parts(int64_t batch, int64_t n, int eb) {
     return deal_row(batch, n, eb, kDistillBlock * kDistillVecs, 2048, kDistillMostVecs);
+}
+
+// 16-byte vectors that a row may take: one more than its bytes need where rows do not all start on a multiple of 16.
+static int64_t vectors_of(const void* x, int64_t n, int64_t stride, rtopk_dtype dt) {
+    const int64_t eb = dt == RTOPK_F32 ? 4 : 2, E = 16 / eb;
+    const bool even = (uintptr_t)x % 16 == 0 && stride % E == 0;
+    return (n + (even ? 0 : E - 1) + E - 1) / E;
+}
+static constexpr int64_t kHeldVecs = 1024 * 20;
+static bool step_is_held(int64_t batch, int64_t vecs) { return vecs <= kHeldVecs && (batch >= 128 || vecs <= 4096); }
+
+template <int DT, int B, int NV>
+static void launch_step(DistillParams P, int64_t batch, hipStream_t st) {
+    const size_t lds = gradient_lds<DT, B, 1>(B * NV);
+    for (P.row0 = 0; P.row0 < batch; P.row0 += kMostWorkgroups) {
+        const dim3 grid((unsigned)(batch - P.row0 < kMostWorkgroups ? batch - P.row0 : kMostWorkgroups));
+        if (P.teacher_lse) hipLaunchKernelGGL((k_distill_step<DT, B, NV, true>), grid, dim3(B), lds, st, P);
+        else hipLaunchKernelGGL((k_distill_step<DT, B, NV, false>), grid, dim3(B), lds, st, P);
+    }
+}
+static rtopk_status launch_held_step(const DistillParams& P, int64_t batch, rtopk_dtype dt, int64_t vecs, hipStream_t st) {
+    (void)hipGetLastError();  // an error left by earlier HIP calls of the process is not this call's
+    return by_type(dt, [&](auto t) {
+        constexpr int DT = decltype(t)::value;
+        if (vecs <= 256 * 4) launch_step<DT, 256, 4>(P, batch, st);
+        else if (vecs <= 256 * 8) launch_step<DT, 256, 8>(P, batch, st);
+        else if (vecs <= 512 * 8) launch_step<DT, 512, 8>(P, batch, st);
+        else if (vecs <= 512 * 16) launch_step<DT, 512, 16>(P, batch, st);
+        else if (vecs <= 1024 * 16) launch_step<DT, 1024, 16>(P, batch, st);
+        else launch_step<DT, 1024, 20>(P, batch, st);
+        return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
+    });
 }
 
 }  // namespace rtopk
@@ -296,9 +517,10 @@ rtopk_status rtopk_distill_backward(const void* student, int64_t batch, int64_t 
     return by_type(dt, [&](auto t) {
         constexpr int DT = decltype(t)::value;
         const int64_t rows = kMostWorkgroups / d.parts > 0 ? kMostWorkgroups / d.parts : 1;
+        const size_t lds = gradient_lds<DT, kDistillGradBlock, kDistillGradVecs>(d.vecs);
         for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
             const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
-            hipLaunchKernelGGL((k_distill_grad<DT>), dim3(now * d.parts), dim3(kDistillGradBlock), k > 1 ? d.vecs : 0, (hipStream_t)hip_stream, P);
+            hipLaunchKernelGGL((k_distill_grad<DT>), dim3(now * d.parts), dim3(kDistillGradBlock), lds, (hipStream_t)hip_stream, P);
         }
         return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
     });
@@ -318,6 +540,18 @@ rtopk_status rtopk_distill_step(const void* student, int64_t batch, int64_t n, i
     if (s != RTOPK_OK) return s;
     if ((uintptr_t)row_weights % 4) return RTOPK_ERR_UNSUPPORTED;
     if (rows_overlap(student, row_stride, out_grad, grad_stride, batch, n, dt == RTOPK_F32 ? 4 : 2)) return RTOPK_ERR_INVALID_ARG;
+    if (step_is_held(batch, vectors_of(student, n, row_stride, dt))) {
+        if (!student || !out_loss) return RTOPK_ERR_INVALID_ARG;
+        s = check_lists(student, batch, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse);
+        if (s != RTOPK_OK) return s;
+        if ((uintptr_t)out_loss % 4 || (uintptr_t)workspace % 256) return RTOPK_ERR_UNSUPPORTED;
+        DistillParams P = distill_params(student, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse);
+        P.loss = out_loss;
+        P.grad_loss = row_weights;
+        P.grad = (char*)out_grad;
+        P.grad_bytes = grad_stride * (dt == RTOPK_F32 ? 4 : 2);
+        return launch_held_step(P, batch, dt, vectors_of(student, n, row_stride, dt), (hipStream_t)hip_stream);
+    }
     float* rows = (float*)((char*)workspace + need - up256((size_t)batch * sizeof(DistillRow)));
     s = rtopk_distill(student, batch, n, row_stride, dt, inv_temperature, teacher_values, teacher_dt, teacher_columns, k, teacher_lse, out_loss, rows, workspace,
                       workspace_bytes, hip_stream);

@@ -85,7 +85,7 @@ constexpr int kGradBlock = 256, kGradVecs = 4;
 
 template <int DT, bool W>
 __global__ void __launch_bounds__(kGradBlock) k_logprobs_grad(LogprobsParams P) {
-    extern __shared__ u32 marks[];
+    extern __shared__ __align__(16) u32 lds[];
     __shared__ u32 twice;
     __shared__ float sums[kGradBlock / 64];
     const u32 part = blockIdx.x % P.parts;
@@ -103,8 +103,8 @@ __global__ void __launch_bounds__(kGradBlock) k_logprobs_grad(LogprobsParams P) 
     const float m = P.row_stats[2 * row], s = P.row_stats[2 * row + 1], ref = finite_or_zero(m);
     const float inv_s = s == 0.0f ? 0.0f : 1.0f / s, log2_s = s == 0.0f ? 0.0f : log2_fast(s);
     const float a = -sum * P.inv_t * inv_s, b = -gh * P.inv_t * kLn2 * inv_s, h2 = W ? P.entropy[row] * (1.0f / kLn2) - log2_s : 0.0f;
-    write_gradient<DT, kGradBlock, kGradVecs, false>(
-        r, out, (((uintptr_t)out ^ (uintptr_t)r.x) & 15) == 0, v0, v1, P.m, marks, &twice, [&](long long i) { return tokens[i]; },
+    write_gradient<DT, kGradBlock, kGradVecs, 1, false>(
+        r, out, (((uintptr_t)out ^ (uintptr_t)r.x) & 15) == 0, v0, v1, P.m, lds, &twice, [&](long long i) { return tokens[i]; },
         [&](long long i) { return g[i]; },
         [&](float x) {
             const float y = (x - ref) * P.c, e = exp2_fast(y);
@@ -243,7 +243,7 @@ rtopk_status rtopk_logprobs_backward(const void* logits, int64_t batch, int64_t 
     return by_type(dt, [&](auto t) {
         constexpr int DT = decltype(t)::value;
         const int64_t rows = kMostWorkgroups / d.parts > 0 ? kMostWorkgroups / d.parts : 1;
-        const size_t lds = m > 1 ? d.vecs : 0;
+        const size_t lds = m > 0 ? gradient_lds<DT, kGradBlock, kGradVecs>(d.vecs) : 0;
         for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
             const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
             if (grad_entropy) hipLaunchKernelGGL((k_logprobs_grad<DT, true>), dim3(now * d.parts), dim3(kGradBlock), lds, (hipStream_t)hip_stream, P);

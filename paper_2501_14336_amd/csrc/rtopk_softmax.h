@@ -47,13 +47,28 @@ struct RowElem {
             }
         }
     }
-    // To the nearest, ties to even; a NaN stays one.
-    __device__ static __forceinline__ u32 to_bits(float x) {
-        if (DT == RTOPK_F32) return __float_as_uint(x);
-        if (DT == RTOPK_F16) return __builtin_bit_cast(uint16_t, (_Float16)x);
-        const u32 b = __float_as_uint(x);
-        return x != x ? 0x7fc0u : (b + 0x7fffu + ((b >> 16) & 1u)) >> 16;
+    // A vector with -inf where `bits` has a bit for the element.
+    __device__ static __forceinline__ u32x4 without(const u32x4& q, u32 bits) {
+        u32x4 r;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            u32 out;  // all ones in the element's bits
+            if constexpr (DT == RTOPK_F32) out = (u32)__builtin_amdgcn_sbfe((int)bits, w, 1);
+            else out = ((u32)__builtin_amdgcn_sbfe((int)bits, 2 * w, 1) & 0xffffu) | ((u32)__builtin_amdgcn_sbfe((int)bits, 2 * w + 1, 1) & 0xffff0000u);
+            r[w] = (q[w] & ~out) | (kMinusInf & out);
+        }
+        return r;
     }
+    // Two numbers to the nearest, ties to even; a NaN stays one.  (One instruction on gfx950.)
+    __device__ static __forceinline__ u32 pack2(float a, float b) {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        const f32x2 v = {a, b};
+        if (DT == RTOPK_F16) return __builtin_bit_cast(u32, __builtin_convertvector(v, f16x2));
+        return __builtin_bit_cast(u32, __builtin_convertvector(v, bf16x2));
+    }
+    __device__ static __forceinline__ u32 to_bits(float x) { return DT == RTOPK_F32 ? __float_as_uint(x) : pack2(x, x) & 0xffffu; }
     __device__ static __forceinline__ void store(char* row, u32 i, float x) {
         if (DT == RTOPK_F32) *(float*)(row + (size_t)i * 4) = x;
         else *(uint16_t*)(row + (size_t)i * 2) = (uint16_t)to_bits(x);
@@ -63,7 +78,7 @@ struct RowElem {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             if constexpr (DT == RTOPK_F32) q[w] = __float_as_uint(x[w]);
-            else q[w] = to_bits(x[2 * w]) | (to_bits(x[2 * w + 1]) << 16);
+            else q[w] = pack2(x[2 * w], x[2 * w + 1]);
         }
         return q;
     }
@@ -144,8 +159,7 @@ __device__ __forceinline__ void sweep_vectors(const RowView<DT>& r, u32 v0, u32 
 
 // ------------------------------------------------------------------------------------------------
 // softmax statistics: m the largest logit, s = sum 2^((x - m) c), w = sum of those terms times their exponents, with c = log2(e) / temperature.
-// m is -inf and s 0 where there is nothing but -inf; a NaN or +inf anywhere makes s NaN, and with it all that is made from it.  (The maximum
-// itself passes over NaNs.)  Everything is kept in 32 bits; a lane adds up a few hundred terms, lanes and waves are joined in a fixed order.
+// m is -inf and s 0 where there is nothing but -inf; a NaN or +inf anywhere makes s NaN, and with it all that is made from it.  Everything is kept in 32 bits; a lane adds up a few hundred terms, lanes and waves are joined in a fixed order.
 // ------------------------------------------------------------------------------------------------
 struct SoftSum {
     float m = -__builtin_inff(), s = 0.0f, w = 0.0f;
@@ -168,13 +182,16 @@ __device__ __forceinline__ void soft_rescale(SoftSum& a, float m, float ref, flo
     a.s *= f;
     a.m = m;
 }
+// The largest of N numbers; NaN if one of them is.  (Two numbers to an instruction, v_maximum3_f32.)
+template <int N>
+__device__ __forceinline__ float largest(float t, const float (&x)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) t = __builtin_elementwise_maximum(t, x[j]);
+    return t;
+}
 template <bool W, int N>
 __device__ __forceinline__ void soft_add(SoftSum& a, const float (&x)[N], float c) {
-    float t = x[0];
-#pragma unroll
-    for (int j = 1; j < N; ++j) t = fmaxf(t, x[j]);
-    t = fmaxf(t, a.m);
-    const float ref = finite_or_zero(t);
+    const float t = largest(a.m, x), ref = finite_or_zero(t);
     soft_rescale<W>(a, t, ref, c);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -185,7 +202,7 @@ __device__ __forceinline__ void soft_add(SoftSum& a, const float (&x)[N], float 
 }
 template <bool W>
 __device__ __forceinline__ SoftSum soft_join(SoftSum a, SoftSum b, float c) {
-    const float m = fmaxf(a.m, b.m), ref = finite_or_zero(m);
+    const float m = __builtin_elementwise_maximum(a.m, b.m), ref = finite_or_zero(m);
     soft_rescale<W>(a, m, ref, c);
     soft_rescale<W>(b, m, ref, c);
     a.s += b.s;
@@ -230,72 +247,183 @@ __device__ __forceinline__ T sum_block(T v, T* sm) {  // likewise
 }
 
 // ------------------------------------------------------------------------------------------------
-// gradients: dense(x) for every element, then the listed columns anew, listed(x, sum of its entries' values).
+// gradients: dense(x) for every element; listed(x, sum of its entries' values) for the columns that a list names.
 // ------------------------------------------------------------------------------------------------
-// Columns are listed in no order and may be listed more than once.  The workgroup marks its own in an LDS bitmap, a byte per vector; where
-// a mark is found set, the whole list is gone through for every entry, lowest entry first, so that sums have one order.
-//   at(i)     the column of entry i, or negative
-//   value(i)  what it adds
-template <int DT, int B, int V, bool NT, class At, class Value, class Dense, class Listed>
-__device__ __forceinline__ void write_gradient(const RowView<DT>& r, char* out, bool aligned, u32 v0, u32 v1, long long entries, u32* marks, u32* twice,
-                                               At&& at, Value&& value, Dense&& dense, Listed&& listed) {
-    constexpr int E = RowElem<DT>::E;
-    auto mine = [&](long long t) {
-        const u64 p = (u64)(t + r.lead) - (u64)v0 * E;  // (wraps below the range)
-        return t >= 0 && t < (long long)r.n && p < (u64)(v1 - v0) * E;
-    };
-    const bool many = entries > 1;
-    if (many) {
+// What a list holds of a workgroup's vectors [v0, v1), in LDS: a bit per column that is listed (a byte per vector), and for one tile at a time the listed columns' gradients, in the
+// tile's order.  The thread that has an entry fetches its logit and works its gradient out; whoever holds the column's vector takes it from there, so that vectors are stored once,
+// whole, and no wave goes through an entry's arithmetic for every column that some lane of it has listed (1024 rows of 131072 bf16, 1024 columns each, loss and gradient:
+// 222 us so).
+//
+// Columns are listed in no order.  Where one is listed more than once (`repeated`), the whole list is gone through for every entry, and the first of a column's has the sum, added up
+// in the list's order.
+//   at(i)      the column of entry i, or negative
+//   value(i)   what is added up
+template <int DT, int B, int V, int R, class At, class Value>
+struct ListedColumns {
+    static constexpr int E = RowElem<DT>::E;
+    static constexpr u32 kTile = B * V * E, kNone = 0xffffffffu;
+    const At& at;
+    const Value& value;
+    long long entries;
+    u64 from, span, lead;  // the workgroup's elements
+    long long n;
+    u32* marks;
+    float* tile;
+    u32 place[R];  // of the thread's first R entries: element of the workgroup's
+    float sum[R];  // ... what is added up, then the column's gradient
+    bool fresh[R];  // ... whether it is the one that marked its column
+    bool any, repeated;
+
+    __device__ __forceinline__ u32 mine(long long t) const {
+        const u64 p = (u64)t + lead - from;  // (wraps below the range)
+        return t >= 0 && t < n && p < span ? (u32)p : kNone;
+    }
+    __device__ __forceinline__ bool mark(u32 p, u32* twice) {
+        if (p == kNone) return false;
+        const u32 v = p / E, bit = 1u << ((v & 3) * 8 + p % E);
+        const bool again = (atomicOr(&marks[v >> 2], bit) & bit) != 0;
+        if (again) *twice = 1;
+        return !again;
+    }
+    // Entry i's place, or none if an entry before it has the same column; the column's sum.
+    __device__ __forceinline__ u32 resolve(long long i, u32 p, float& all) const {
+        if (p == kNone || !repeated) return p;
+        const long long t = at(i);
+        all = 0.0f;
+        for (long long l = 0; l < entries; ++l)
+            if (at(l) == t) {
+                if (l < i) return kNone;
+                all += value(l);
+            }
+        return p;
+    }
+    // All threads of the workgroup.  own(k, column, value): the thread's k-th entry; marked(p): called once for every listed column that no thread's first R entries have.
+    template <class Own, class Marked>
+    __device__ __forceinline__ ListedColumns(const RowView<DT>& r, u32 v0, u32 v1, long long entries_, u32* lds, u32* twice, const At& at_, const Value& value_, Own&& own, Marked&& marked)
+        : at(at_), value(value_), entries(entries_), from((u64)v0 * E), span((u64)(v1 - v0) * E), lead(r.lead), n(r.n), marks(lds), tile((float*)(lds + ((v1 - v0 + 15) / 16) * 4)),
+          any(false), repeated(false) {
+        if (entries == 0) return;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            long long t = -1;
+            sum[k] = 0.0f;
+            fresh[k] = false;
+            if (threadIdx.x + (long long)k * B < entries) own(k, t, sum[k]);
+            place[k] = mine(t);
+            any |= place[k] != kNone;
+        }
+        for (long long i = threadIdx.x + (long long)R * B; i < entries; i += B) any |= mine(at(i)) != kNone;
         for (u32 i = threadIdx.x; i < (v1 - v0 + 3) / 4; i += B) marks[i] = 0;
         if (threadIdx.x == 0) *twice = 0;
+        any = __syncthreads_or(any);
+        if (!any) return;
+#pragma unroll
+        for (int k = 0; k < R; ++k) fresh[k] = mark(place[k], twice);
+        for (long long i = threadIdx.x + (long long)R * B; i < entries; i += B) {
+            const u32 p = mine(at(i));
+            if (mark(p, twice)) marked(p);
+        }
         __syncthreads();
-        for (long long i = threadIdx.x; i < entries; i += B) {
-            const long long t = at(i);
-            if (mine(t)) {
-                const u32 p = (u32)(t + r.lead - (long long)v0 * E), v = p / E, bit = 1u << ((v & 3) * 8 + p % E);
-                if (atomicOr(&marks[v >> 2], bit) & bit) *twice = 1;
-            }
+        repeated = *twice != 0;
+    }
+    // listed(k, p, sum): the gradient of the column at p, whose entries add up to sum; k: which of the thread's first R entries it is, or negative.
+    template <class Listed>
+    __device__ __forceinline__ void work_out(Listed&& listed) {
+        if (!any) return;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            place[k] = resolve(threadIdx.x + (long long)k * B, place[k], sum[k]);
+            if (place[k] != kNone) sum[k] = listed(k, place[k], sum[k]);
         }
     }
+    // The gradients of the tile that begins at the workgroup's element `first`; a barrier has to follow.
+    template <class Listed>
+    __device__ __forceinline__ void put(u32 first, Listed&& listed) {
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (place[k] != kNone && place[k] - first < kTile) tile[place[k] - first] = sum[k];
+        for (long long i = threadIdx.x + (long long)R * B; i < entries; i += B) {
+            u32 p = mine(at(i));
+            if (p == kNone || p - first >= kTile) continue;
+            float all = value(i);
+            p = resolve(i, p, all);
+            if (p != kNone) tile[p - first] = listed(-1, p, all);
+        }
+    }
+    __device__ __forceinline__ u32 listed_of(u32 v) const { return ((const uint8_t*)marks)[v]; }  // bits of the workgroup's vector v
+};
+// Bytes of LDS for a list: the marks of a part's vectors, a tile's gradients.
+template <int DT, int B, int V>
+static inline size_t gradient_lds(u32 vecs) { return (((size_t)vecs + 15) & ~(size_t)15) + (size_t)B * V * RowElem<DT>::E * 4; }
+
+// dense(x) of a vector, and what `tile` has for its listed columns.
+template <int DT, class Dense>
+__device__ __forceinline__ void gradient_of_vector(float (&x)[RowElem<DT>::E], u32 bits, const float* tile, Dense&& dense) {
+    constexpr int E = RowElem<DT>::E;
+#pragma unroll
+    for (int j = 0; j < E; ++j) x[j] = dense(x[j]);
+    if (bits != 0) {
+        float t[E];
+#pragma unroll
+        for (int h = 0; h < E / 4; ++h) {
+            const float4 w = ((const float4*)tile)[h];
+            t[4 * h] = w.x;
+            t[4 * h + 1] = w.y;
+            t[4 * h + 2] = w.z;
+            t[4 * h + 3] = w.w;
+        }
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = (bits >> j) & 1 ? t[j] : x[j];
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ void store_vector(const RowView<DT>& r, char* out, bool aligned, u32 v, const float (&x)[RowElem<DT>::E]) {
+    constexpr int E = RowElem<DT>::E;
+    if (aligned && r.whole(v)) {
+        typedef __attribute__((address_space(1))) u32x4* vec_out;
+        *(vec_out)(out + ((long long)v * E - r.lead) * RowElem<DT>::kBytes) = RowElem<DT>::pack(x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const u32 col = v * E + j - r.lead;
+            if (col < r.n) RowElem<DT>::store(out, col, x[j]);
+        }
+    }
+}
+
+// `aligned`: the output's row starts where the input's does within 16 bytes.  lds: gradient_lds() bytes, where there are entries.  listed(x, sum): the gradient of a listed column.
+template <int DT, int B, int V, int R, bool NT, class At, class Value, class Dense, class Listed>
+__device__ __forceinline__ void write_gradient(const RowView<DT>& r, char* out, bool aligned, u32 v0, u32 v1, long long entries, u32* lds, u32* twice, const At& at, const Value& value,
+                                               Dense&& dense, Listed&& listed) {
+    constexpr int E = RowElem<DT>::E;
+    ListedColumns<DT, B, V, R, At, Value> list(
+        r, v0, v1, entries, lds, twice, at, value,
+        [&](int k, long long& t, float& v) {
+            const long long i = threadIdx.x + (long long)k * B;
+            t = at(i);
+            if (t >= 0) v = value(i);
+        },
+        [](u32) {});
+    auto of_column = [&](int, u32 p, float sum) { return listed(RowElem<DT>::load(r.x, p + v0 * E - r.lead), sum); };
+    list.work_out(of_column);
     sweep_vectors<DT, B, V, NT>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
+        if (list.any) {
+            list.put((first - v0) * E, of_column);
+            __syncthreads();
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const u32 v = first + i * B + threadIdx.x;
             if (v < v1) {
                 float x[E];
                 RowElem<DT>::unpack(q[i], x);
-#pragma unroll
-                for (int j = 0; j < E; ++j) x[j] = dense(x[j]);
-                if (aligned && r.whole(v)) {
-                    typedef __attribute__((address_space(1))) u32x4* vec_out;
-                    *(vec_out)(out + ((long long)v * E - r.lead) * RowElem<DT>::kBytes) = RowElem<DT>::pack(x);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const u32 col = v * E + j - r.lead;
-                        if (col < r.n) RowElem<DT>::store(out, col, x[j]);
-                    }
-                }
+                gradient_of_vector<DT>(x, list.any ? list.listed_of(v - v0) : 0, list.tile + (i * B + threadIdx.x) * E, dense);
+                store_vector<DT>(r, out, aligned, v, x);
             }
         }
+        if (list.any) __syncthreads();  // (before the next tile's gradients)
     });
-    __syncthreads();  // (and what was stored is there: a listed column is written after the dense one)
-    const bool repeated = many && *twice != 0;
-    for (long long i = threadIdx.x; i < entries; i += B) {
-        const long long t = at(i);
-        if (!mine(t)) continue;
-        float sum = value(i);
-        bool first = true;
-        if (repeated) {
-            sum = 0.0f;
-            for (long long l = 0; l < entries; ++l)
-                if (at(l) == t) {
-                    if (l < i) first = false;
-                    sum += value(l);
-                }
-        }
-        if (first) RowElem<DT>::store(out, (u32)t, listed(RowElem<DT>::load(r.x, (u32)t), sum));
-    }
 }
 
 // ------------------------------------------------------------------------------------------------
