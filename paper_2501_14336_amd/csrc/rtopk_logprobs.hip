@@ -103,12 +103,20 @@ __global__ void __launch_bounds__(kGradBlock) k_logprobs_grad(LogprobsParams P) 
     const float m = P.row_stats[2 * row], s = P.row_stats[2 * row + 1], ref = finite_or_zero(m);
     const float inv_s = s == 0.0f ? 0.0f : 1.0f / s, log2_s = s == 0.0f ? 0.0f : log2_fast(s);
     const float a = -sum * P.inv_t * inv_s, b = -gh * P.inv_t * kLn2 * inv_s, h2 = W ? P.entropy[row] * (1.0f / kLn2) - log2_s : 0.0f;
+    const ScaledExp<DT> dense(a, ref, P.c);
     write_gradient<DT, kGradBlock, kGradVecs, 1, false>(
         r, out, (((uintptr_t)out ^ (uintptr_t)r.x) & 15) == 0, v0, v1, P.m, lds, &twice, [&](long long i) { return tokens[i]; },
         [&](long long i) { return g[i]; },
-        [&](float x) {
-            const float y = (x - ref) * P.c, e = exp2_fast(y);
-            return W ? e * (a + b * (fmaxf(y, kNothing) + h2)) : e * a;
+        [&](float (&x)[RowElem<DT>::E]) {
+            if (!W) {
+                dense.of(x);
+                return;
+            }
+#pragma unroll
+            for (int j = 0; j < RowElem<DT>::E; ++j) {
+                const float y = (x[j] - ref) * P.c;
+                x[j] = exp2_fast(y) * (a + b * (fmaxf(y, kNothing) + h2));
+            }
         },
         [&](float x, float gi) {
             const float y = (x - ref) * P.c, e = exp2_fast(y);

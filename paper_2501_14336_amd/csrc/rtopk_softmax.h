@@ -13,6 +13,9 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 // Below this many powers of two a term is zero in 32 bits, and so is its product with its own logarithm.  (Where a masked logit makes the logarithm infinite the product would be NaN.)
 constexpr float kNothing = -200.0f;
 
+// A number that is the same in all of a wave's lanes, kept once.
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
 
@@ -193,6 +196,16 @@ template <bool W, int N>
 __device__ __forceinline__ void soft_add(SoftSum& a, const float (&x)[N], float c) {
     const float t = largest(a.m, x), ref = finite_or_zero(t);
     soft_rescale<W>(a, t, ref, c);
+    // The exponent in one fused step, x c - r with r the rounded ref c; the sum is put right for what that rounding took off.  (Not where ref c leaves the range: logits at a type's lowest
+    // or highest values.)
+    const float r = ref * c, off = __builtin_fmaf(ref, c, -r);
+    if (!W && ballot64(!(fabsf(r) < 1e30f)) == 0) {
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) s += exp2_fast(__builtin_fmaf(x[j], c, -r));
+        a.s += s * exp2_fast(-off);
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const float y = (x[j] - ref) * c, e = exp2_fast(y);
@@ -247,7 +260,7 @@ __device__ __forceinline__ T sum_block(T v, T* sm) {  // likewise
 }
 
 // ------------------------------------------------------------------------------------------------
-// gradients: dense(x) for every element; listed(x, sum of its entries' values) for the columns that a list names.
+// gradients: dense(x) for the elements of a vector; listed(x, sum of its entries' values) for the columns that a list names.
 // ------------------------------------------------------------------------------------------------
 // What a list holds of a workgroup's vectors [v0, v1), in LDS: a bit per column that is listed (a byte per vector), and for one tile at a time the listed columns' gradients, in the
 // tile's order.  The thread that has an entry fetches its logit and works its gradient out; whoever holds the column's vector takes it from there, so that vectors are stored once,
@@ -297,11 +310,18 @@ struct ListedColumns {
             }
         return p;
     }
+    // All threads of the workgroup, before the list is read; a barrier has to lie between.
+    static __device__ __forceinline__ void clear(u32 vecs, u32* lds, u32* twice) {
+        for (u32 i = threadIdx.x; i < (vecs + 3) / 4; i += B) lds[i] = 0;
+        if (threadIdx.x == 0) *twice = 0;
+    }
     // All threads of the workgroup.  own(k, column, value): the thread's k-th entry; marked(p): called once for every listed column that no thread's first R entries have.
-    template <class Own, class Marked>
-    __device__ __forceinline__ ListedColumns(const RowView<DT>& r, u32 v0, u32 v1, long long entries_, u32* lds, u32* twice, const At& at_, const Value& value_, Own&& own, Marked&& marked)
+    // WHOLE: the workgroup has the whole row, whose list is not looked through for entries that are not its own, and has been cleared for.
+    template <bool WHOLE, class Own, class Marked>
+    __device__ __forceinline__ ListedColumns(std::integral_constant<bool, WHOLE>, const RowView<DT>& r, u32 v0, u32 v1, long long entries_, u32* lds, u32* twice, const At& at_,
+                                             const Value& value_, Own&& own, Marked&& marked)
         : at(at_), value(value_), entries(entries_), from((u64)v0 * E), span((u64)(v1 - v0) * E), lead(r.lead), n(r.n), marks(lds), tile((float*)(lds + ((v1 - v0 + 15) / 16) * 4)),
-          any(false), repeated(false) {
+          any(WHOLE), repeated(false) {
         if (entries == 0) return;
 #pragma unroll
         for (int k = 0; k < R; ++k) {
@@ -312,11 +332,12 @@ struct ListedColumns {
             place[k] = mine(t);
             any |= place[k] != kNone;
         }
-        for (long long i = threadIdx.x + (long long)R * B; i < entries; i += B) any |= mine(at(i)) != kNone;
-        for (u32 i = threadIdx.x; i < (v1 - v0 + 3) / 4; i += B) marks[i] = 0;
-        if (threadIdx.x == 0) *twice = 0;
-        any = __syncthreads_or(any);
-        if (!any) return;
+        if (!WHOLE) {
+            for (long long i = threadIdx.x + (long long)R * B; i < entries; i += B) any |= mine(at(i)) != kNone;
+            clear(v1 - v0, lds, twice);
+            any = __syncthreads_or(any);
+            if (!any) return;
+        }
 #pragma unroll
         for (int k = 0; k < R; ++k) fresh[k] = mark(place[k], twice);
         for (long long i = threadIdx.x + (long long)R * B; i < entries; i += B) {
@@ -336,18 +357,18 @@ struct ListedColumns {
             if (place[k] != kNone) sum[k] = listed(k, place[k], sum[k]);
         }
     }
-    // The gradients of the tile that begins at the workgroup's element `first`; a barrier has to follow.
+    // The gradients of the tile that begins at the workgroup's element `first`, into the tile at `to`; a barrier has to follow.
     template <class Listed>
-    __device__ __forceinline__ void put(u32 first, Listed&& listed) {
+    __device__ __forceinline__ void put(u32 first, float* to, Listed&& listed) {
 #pragma unroll
         for (int k = 0; k < R; ++k)
-            if (place[k] != kNone && place[k] - first < kTile) tile[place[k] - first] = sum[k];
+            if (place[k] != kNone && place[k] - first < kTile) to[place[k] - first] = sum[k];
         for (long long i = threadIdx.x + (long long)R * B; i < entries; i += B) {
             u32 p = mine(at(i));
             if (p == kNone || p - first >= kTile) continue;
             float all = value(i);
             p = resolve(i, p, all);
-            if (p != kNone) tile[p - first] = listed(-1, p, all);
+            if (p != kNone) to[p - first] = listed(-1, p, all);
         }
     }
     __device__ __forceinline__ u32 listed_of(u32 v) const { return ((const uint8_t*)marks)[v]; }  // bits of the workgroup's vector v
@@ -356,12 +377,33 @@ struct ListedColumns {
 template <int DT, int B, int V>
 static inline size_t gradient_lds(u32 vecs) { return (((size_t)vecs + 15) & ~(size_t)15) + (size_t)B * V * RowElem<DT>::E * 4; }
 
-// dense(x) of a vector, and what `tile` has for its listed columns.
-template <int DT, class Dense>
-__device__ __forceinline__ void gradient_of_vector(float (&x)[RowElem<DT>::E], u32 bits, const float* tile, Dense&& dense) {
+// a 2^((x - ref) c) for the elements of a vector, in two instructions each.
+//   16-bit types: the factor is in the exponent, which is rounded to 2^-20 or so there; 32 bits: it is a product.  Where ref c leaves the range (logits at a type's lowest or highest
+//   values) the difference is taken first.
+template <int DT>
+struct ScaledExp {
+    float c, r, a, ref;
+    bool plain, sign;
+    __device__ __forceinline__ ScaledExp(float scale, float ref_, float c_) : c(c_), ref(uniform(ref_)) {
+        const float p = ref_ * c_, off = __builtin_fmaf(ref_, c_, -p);
+        plain = __builtin_amdgcn_readfirstlane(fabsf(p) < 1e30f) != 0;
+        sign = __builtin_amdgcn_readfirstlane(DT != RTOPK_F32 && scale < 0.0f) != 0;
+        if (DT == RTOPK_F32) {
+            r = uniform(p);
+            a = uniform(plain ? scale * exp2_fast(-off) : scale);
+        } else {
+            const float l = log2_fast(fabsf(scale));
+            r = uniform(plain ? p - l : -l);
+            a = 1.0f;
+        }
+    }
+    __device__ __forceinline__ void of(float (&x)[RowElem<DT>::E]) const;
+};
+
+// What `tile` has for a vector's listed columns.
+template <int DT>
+__device__ __forceinline__ void listed_gradients(float (&x)[RowElem<DT>::E], u32 bits, const float* tile) {
     constexpr int E = RowElem<DT>::E;
-#pragma unroll
-    for (int j = 0; j < E; ++j) x[j] = dense(x[j]);
     if (bits != 0) {
         float t[E];
 #pragma unroll
@@ -374,6 +416,25 @@ __device__ __forceinline__ void gradient_of_vector(float (&x)[RowElem<DT>::E], u
         }
 #pragma unroll
         for (int j = 0; j < E; ++j) x[j] = (bits >> j) & 1 ? t[j] : x[j];
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ void ScaledExp<DT>::of(float (&x)[RowElem<DT>::E]) const {
+    constexpr int E = RowElem<DT>::E;
+    if (__builtin_expect(plain, 1)) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, -r));
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = exp2_fast((x[j] - ref) * c - (DT == RTOPK_F32 ? 0.0f : r));
+    }
+    if (DT == RTOPK_F32) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] *= a;
+    } else if (sign) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = -x[j];
     }
 }
 
@@ -398,7 +459,7 @@ __device__ __forceinline__ void write_gradient(const RowView<DT>& r, char* out, 
                                                Dense&& dense, Listed&& listed) {
     constexpr int E = RowElem<DT>::E;
     ListedColumns<DT, B, V, R, At, Value> list(
-        r, v0, v1, entries, lds, twice, at, value,
+        std::false_type{}, r, v0, v1, entries, lds, twice, at, value,
         [&](int k, long long& t, float& v) {
             const long long i = threadIdx.x + (long long)k * B;
             t = at(i);
@@ -409,7 +470,7 @@ __device__ __forceinline__ void write_gradient(const RowView<DT>& r, char* out, 
     list.work_out(of_column);
     sweep_vectors<DT, B, V, NT>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
         if (list.any) {
-            list.put((first - v0) * E, of_column);
+            list.put((first - v0) * E, list.tile, of_column);
             __syncthreads();
         }
 #pragma unroll
@@ -418,7 +479,8 @@ __device__ __forceinline__ void write_gradient(const RowView<DT>& r, char* out, 
             if (v < v1) {
                 float x[E];
                 RowElem<DT>::unpack(q[i], x);
-                gradient_of_vector<DT>(x, list.any ? list.listed_of(v - v0) : 0, list.tile + (i * B + threadIdx.x) * E, dense);
+                dense(x);
+                listed_gradients<DT>(x, list.any ? list.listed_of(v - v0) : 0, list.tile + (i * B + threadIdx.x) * E);
                 store_vector<DT>(r, out, aligned, v, x);
             }
         }
