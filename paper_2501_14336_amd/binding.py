@@ -105,8 +105,8 @@ class RtopkError(RuntimeError):
 
 _SOURCES = ("rtopk_api.hip", "rtopk_f32.hip", "rtopk_f16.hip", "rtopk_bf16.hip", "rtopk_list_f32.hip", "rtopk_list_f16.hip",
             "rtopk_list_bf16.hip", "rtopk_rows_f32.hip", "rtopk_rows_f16.hip", "rtopk_rows_bf16.hip",
-            "rtopk_logprobs.hip", "rtopk_distill.hip", "rtopk_route.hip")
-_HEADERS = ("rtopk_device.h", "rtopk_host.h", "rtopk_softmax.h", "rtopk_kernels.inl", "rtopk_sort.inl", "rtopk_list.inl")
+            "rtopk_logprobs.hip", "rtopk_distill.hip", "rtopk_distill_f32.hip", "rtopk_distill_f16.hip", "rtopk_distill_bf16.hip", "rtopk_route.hip")
+_HEADERS = ("rtopk_device.h", "rtopk_host.h", "rtopk_softmax.h", "rtopk_distill.h", "rtopk_distill_step.inl", "rtopk_kernels.inl", "rtopk_sort.inl", "rtopk_list.inl")
 
 
 def build(force: bool = True) -> str:

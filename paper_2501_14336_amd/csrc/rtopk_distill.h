@@ -1,0 +1,74 @@
+// What the distillation kernels share (rtopk_distill.hip, rtopk_distill_step.inl).
+#pragma once
+#include "rtopk_softmax.h"
+
+namespace rtopk {
+
+// What a row's forward pass leaves for its gradient.  p_j = exp((x_j - m) / T) / s.
+struct DistillRow {
+    float m, s;        // the student's maximum and sum
+    float zref, zmul;  // q_i = exp((z_i - zref) / T) * zmul, or exp(z_i / T - zref) with the teacher's log-sum
+    float mu, dense;   // columns not listed: dx = (g / T) exp((x - mu) / T) dense
+    float q, spare;    // sum q + r
+};
+static_assert(sizeof(DistillRow) == RTOPK_DISTILL_ROW_STATS * sizeof(float), "as declared");
+
+struct DistillParams {
+    const char* student;
+    long long row_bytes, row0, batch, k;
+    u32 n, parts, part_vecs;
+    float c, inv_t;
+    const void* values;         // [batch][k], type value_dt
+    int value_dt;
+    const long long* columns;   // [batch][k]
+    const float* teacher_lse;   // [batch], or null
+    float4* partial;            // [batch][parts][2]: columns not listed, listed columns
+    float* loss;
+    DistillRow* rows;
+    // the gradient
+    const float* grad_loss;
+    char* grad;
+    long long grad_bytes;
+};
+
+// ln of an entry's share.
+__device__ __forceinline__ float ln_share(float z, const DistillRow& d, bool tail, float ln_zmul, float inv_t) {
+    return tail ? z * inv_t - d.zref : (z - d.zref) * inv_t + ln_zmul;
+}
+
+// A row's statistics from the sums of all its columns (a), of those that are not listed (others), of the teacher's list (zs), and of its shares (share): fills d, whose zref and zmul
+// are there, and returns the rest's part of the loss.
+template <bool TAIL>
+__device__ __forceinline__ float finish_row(DistillRow& d, const SoftSum& a, const SoftSum& others, double share, float zs, const DistillParams& P) {
+    d.m = a.m;
+    d.s = a.s;
+    d.spare = 0.0f;
+    if (!TAIL) {
+        d.q = zs == 0.0f ? 0.0f : zs != zs ? zs : 1.0f;
+        d.mu = finite_or_zero(a.m);
+        d.dense = a.s == 0.0f ? 0.0f : d.q / a.s;
+        return 0.0f;
+    }
+    const float rest = share < 1.0 ? (float)(1.0 - share) : share != share ? (float)share : 0.0f;
+    const float ln_other = others.s == 0.0f ? -__builtin_inff() : (others.m - a.m) * P.inv_t + kLn2 * (log2_fast(others.s) - log2_fast(a.s));
+    d.q = share < 1.0 ? 1.0f : (float)share;
+    d.mu = finite_or_zero(others.m);
+    d.dense = others.s == 0.0f ? 0.0f : d.q * exp2_fast((d.mu - finite_or_zero(a.m)) * P.c) / a.s - rest / others.s;
+    return rest != 0.0f ? rest * (kLn2 * log2_fast(rest) - ln_other) : 0.0f;
+}
+
+// An entry's share under the teacher's log-sum, without the rounding of its logarithm: what all of them leave of 1 may be a millionth.
+__device__ __forceinline__ double exact_share(float z, float lse, float inv_t) {
+    const float p = z * inv_t, low = __builtin_fmaf(z, inv_t, -p), hi = p - lse, back = hi - p;  // p + low is z inv_t exactly; hi + rest is p - lse exactly
+    const float rest = (p - (hi - back)) + (-lse - back);
+    const double e = (double)expf(hi);
+    return fabsf(hi) < 1e30f ? e * (1.0 + (double)(low + rest)) : e;  // (a masked entry has none to add)
+}
+
+// Loss and gradient in one launch, for rows of up to kHeldVecs vectors of 16 bytes (defined in rtopk_distill_f32.hip / rtopk_distill_f16.hip / rtopk_distill_bf16.hip).
+constexpr int64_t kHeldVecs = 1024 * 20;
+rtopk_status launch_distill_step_f32(const DistillParams& P, int64_t vecs, hipStream_t st);
+rtopk_status launch_distill_step_f16(const DistillParams& P, int64_t vecs, hipStream_t st);
+rtopk_status launch_distill_step_bf16(const DistillParams& P, int64_t vecs, hipStream_t st);
+
+}  // namespace rtopk

@@ -1,0 +1,6 @@
+// Distillation in one launch, for RTOPK_BF16 logits.
+#include "rtopk_distill_step.inl"
+
+namespace rtopk {
+rtopk_status launch_distill_step_bf16(const DistillParams& P, int64_t vecs, hipStream_t st) { return launch_step_of<RTOPK_BF16>(P, vecs, st); }
+}  // namespace rtopk

@@ -222,10 +222,11 @@ __device__ __forceinline__ SoftSum soft_join(SoftSum a, SoftSum b, float c) {
     if (W) a.w += b.w;
     return a;
 }
-template <bool W>
-__device__ __forceinline__ SoftSum soft_wave(SoftSum a, float c) {  // the same in every lane
+// Over LANES lanes that follow one another, the same in all of them.
+template <bool W, int LANES = 64>
+__device__ __forceinline__ SoftSum soft_wave(SoftSum a, float c) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
+    for (int d = 1; d < LANES; d *= 2) {
         SoftSum b;
         b.m = __shfl_xor(a.m, d);
         b.s = __shfl_xor(a.s, d);
@@ -234,17 +235,15 @@ __device__ __forceinline__ SoftSum soft_wave(SoftSum a, float c) {  // the same 
     }
     return a;
 }
-// Over the workgroup, the same in every thread.  `sm` has an entry per wave; it may be used again after the next barrier.
+// Over the workgroup, the same in every thread.  `sm` has an entry per wave; it may be used again after the next barrier.  (Waves' sums are joined across lanes: read by every lane,
+// those of 16 waves would take 64 registers.)
 template <int B, bool W>
 __device__ __forceinline__ SoftSum soft_block(SoftSum a, float c, float4* sm) {
     a = soft_wave<W>(a, c);
     if constexpr (B == 64) return a;
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = packed(a);
     __syncthreads();
-    a = unpacked(sm[0]);
-#pragma unroll
-    for (int i = 1; i < B / 64; ++i) a = soft_join<W>(a, unpacked(sm[i]), c);
-    return a;
+    return soft_wave<W, B / 64>(unpacked(sm[threadIdx.x % (B / 64)]), c);
 }
 template <int B, class T>
 __device__ __forceinline__ T sum_block(T v, T* sm) {  // likewise
@@ -253,9 +252,9 @@ __device__ __forceinline__ T sum_block(T v, T* sm) {  // likewise
     if constexpr (B == 64) return v;
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = sm[0];
+    v = sm[threadIdx.x % (B / 64)];
 #pragma unroll
-    for (int i = 1; i < B / 64; ++i) v += sm[i];
+    for (int d = 1; d < B / 64; d *= 2) v += __shfl_xor(v, d);
     return v;
 }
 
