@@ -10,26 +10,75 @@
 
 namespace rtopk {
 
-constexpr int kDistillBlock = 256, kDistillVecs = 4;
+// The loss of a row, and what its gradient needs of it, from the sums of its columns (TAIL: of those that are not listed, and of those that are).
+template <int DT, bool TAIL, int B>
+__device__ __forceinline__ void loss_of_row(const DistillParams& P, long long row, const RowView<DT>& r, SoftSum a, const SoftSum& listed, float4* sm, double* sums) {
+    const long long* columns = P.columns + row * P.k;
+    const SoftSum others = a;
+    if (TAIL) a = soft_join<false>(a, listed, P.c);
+    DistillRow d;
+    float ln_zmul = 0.0f, zs = 1.0f;
+    if (TAIL) {
+        d.zref = P.teacher_lse[row];
+        d.zmul = 1.0f;
+    } else {
+        SoftSum z;
+        for (long long i = threadIdx.x; i < P.k; i += B)
+            if (columns[i] >= 0) {
+                const float v[1] = {load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i))};
+                soft_add<false>(z, v, P.c);
+            }
+        z = soft_block<B, false>(z, P.c, sm);
+        zs = z.s;
+        d.zref = finite_or_zero(z.m);
+        d.zmul = zs == 0.0f ? 0.0f : 1.0f / zs;
+        ln_zmul = zs == 0.0f ? 0.0f : -kLn2 * log2_fast(zs);
+    }
+    const float ln_s = kLn2 * log2_fast(a.s);
+    float loss = 0.0f;
+    double share = 0.0;
+    for (long long i = threadIdx.x; i < P.k; i += B) {
+        const long long t = columns[i];
+        if (t < 0) continue;
+        const float z = load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i)), lq = ln_share(z, d, TAIL, ln_zmul, P.inv_t), qi = expf(lq);
+        if (TAIL) share += exact_share(z, d.zref, P.inv_t);
+        if (t >= (long long)P.n) {
+            loss += __builtin_nanf("");
+        } else if (qi != 0.0f) {
+            const float x = RowElem<DT>::load(r.x, (u32)t);
+            loss += qi * (lq - (a.s == 0.0f ? -__builtin_inff() : (x - a.m) * P.inv_t - ln_s));
+        }
+    }
+    loss = sum_block<B>(loss, (float*)sums);
+    if (TAIL) share = sum_block<B>(share, sums + B / 64);
+    loss += finish_row<TAIL>(d, a, others, share, zs, P);
+    if (threadIdx.x == 0) {
+        P.loss[row] = loss;
+        if (P.rows) P.rows[row] = d;
+    }
+}
 
-// Statistics of a part of a row; TAIL: apart for columns that are listed and for the others.
-template <int DT, bool TAIL>
-__global__ void __launch_bounds__(kDistillBlock) k_distill_part(DistillParams P) {
+constexpr int kDistillVecs = 4;
+
+// Statistics of a row, or of a part of one; TAIL: apart for columns that are listed and for the others.  WHOLE: of the row, and its loss.
+template <int DT, bool TAIL, int B, bool WHOLE>
+__global__ void __launch_bounds__(B) k_distill_part(DistillParams P) {
     extern __shared__ u32 marks[];  // TAIL: a byte per vector of the part, a bit per column
-    __shared__ float4 sm[kDistillBlock / 64];
-    constexpr int E = RowElem<DT>::E;
-    const u32 part = blockIdx.x % P.parts;
-    const long long row = P.row0 + blockIdx.x / P.parts;
+    __shared__ float4 sm[3][B / 64];
+    __shared__ double sums[2 * B / 64];
+    constexpr int E = RowElem<DT>::E, V = kDistillVecs;
+    const u32 part = WHOLE ? 0u : blockIdx.x % P.parts;
+    const long long row = P.row0 + (WHOLE ? blockIdx.x : blockIdx.x / P.parts);
     const RowView<DT> r(P.student, row, P.row_bytes, P.n);
     const u32 v0 = part * P.part_vecs, v1 = part_end(v0, P.part_vecs, r.nvec);
     SoftSum a, listed;
     if (TAIL) {
         const long long* columns = P.columns + row * P.k;
-        for (u32 i = threadIdx.x; i < (P.part_vecs + 3) / 4; i += kDistillBlock) marks[i] = 0;
+        for (u32 i = threadIdx.x; i < (P.part_vecs + 3) / 4; i += B) marks[i] = 0;
         __syncthreads();
-        for (long long i = threadIdx.x; i < P.k; i += kDistillBlock) {
+        for (long long i = threadIdx.x; i < P.k; i += B) {
             const long long t = columns[i];
-            const u64 p = (u64)(t + r.lead) - (u64)v0 * E;  // (wraps below the part)
+            const u64 p = (u64)t + r.lead - (u64)v0 * E;  // (wraps below the part)
             if (t >= 0 && t < (long long)P.n && p < (u64)(v1 - v0) * E) {
                 const u32 v = (u32)p / E, bit = 1u << ((v & 3) * 8 + (u32)p % E);
                 if (!(atomicOr(&marks[v >> 2], bit) & bit)) {  // a column listed twice counts once
@@ -40,13 +89,13 @@ __global__ void __launch_bounds__(kDistillBlock) k_distill_part(DistillParams P)
         }
         __syncthreads();
     }
-    sweep_vectors<DT, kDistillBlock, kDistillVecs, false>(r, v0, v1, [&](const u32x4 (&q)[kDistillVecs], u32 first) {
-        float x[kDistillVecs * E];
+    sweep_vectors<DT, B, V, false>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
+        float x[V * E];
 #pragma unroll
-        for (int i = 0; i < kDistillVecs; ++i) {
+        for (int i = 0; i < V; ++i) {
             u32 bits = 0;
             if (TAIL) {
-                const u32 v = first + i * kDistillBlock + threadIdx.x;
+                const u32 v = first + i * B + threadIdx.x;
                 if (v < v1) bits = ((const uint8_t*)marks)[v - v0];
             }
             float y[E];
@@ -56,71 +105,32 @@ __global__ void __launch_bounds__(kDistillBlock) k_distill_part(DistillParams P)
         }
         soft_add<false>(a, x, P.c);
     });
-    a = soft_block<kDistillBlock, false>(a, P.c, sm);
-    if (threadIdx.x == 0) P.partial[(row * P.parts + part) * 2] = packed(a);
-    if (TAIL) {
-        __syncthreads();
-        listed = soft_block<kDistillBlock, false>(listed, P.c, sm);
-        if (threadIdx.x == 0) P.partial[(row * P.parts + part) * 2 + 1] = packed(listed);
+    a = soft_block<B, false>(a, P.c, sm[0]);
+    if (TAIL) listed = soft_block<B, false>(listed, P.c, sm[1]);
+    if (WHOLE) {
+        loss_of_row<DT, TAIL, B>(P, row, r, a, listed, sm[2], sums);
+    } else if (threadIdx.x == 0) {
+        P.partial[(row * P.parts + part) * 2] = packed(a);
+        if (TAIL) P.partial[(row * P.parts + part) * 2 + 1] = packed(listed);
     }
 }
 
 constexpr int kDistillFinish = 256;
 
-template <int DT>
+template <int DT, bool TAIL>
 __global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams P) {
     __shared__ float4 sm[3][kDistillFinish / 64];
-    __shared__ double sums[2][kDistillFinish / 64];
+    __shared__ double sums[2 * kDistillFinish / 64];
     const long long row = P.row0 + blockIdx.x;
-    const bool tail = P.teacher_lse != nullptr;
     const RowView<DT> r(P.student, row, P.row_bytes, P.n);
-    const long long* columns = P.columns + row * P.k;
-    SoftSum a, listed, z;
+    SoftSum a, listed;
     for (u32 i = threadIdx.x; i < P.parts; i += kDistillFinish) {
         a = soft_join<false>(a, unpacked(P.partial[(row * P.parts + i) * 2]), P.c);
-        if (tail) listed = soft_join<false>(listed, unpacked(P.partial[(row * P.parts + i) * 2 + 1]), P.c);
+        if (TAIL) listed = soft_join<false>(listed, unpacked(P.partial[(row * P.parts + i) * 2 + 1]), P.c);
     }
     a = soft_block<kDistillFinish, false>(a, P.c, sm[0]);
-    const SoftSum others = a;
-    if (tail) a = soft_join<false>(a, soft_block<kDistillFinish, false>(listed, P.c, sm[1]), P.c);
-    DistillRow d;
-    float ln_zmul = 0.0f;
-    if (tail) {
-        d.zref = P.teacher_lse[row];
-        d.zmul = 1.0f;
-    } else {
-        for (long long i = threadIdx.x; i < P.k; i += kDistillFinish)
-            if (columns[i] >= 0) {
-                const float v[1] = {load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i))};
-                soft_add<false>(z, v, P.c);
-            }
-        z = soft_block<kDistillFinish, false>(z, P.c, sm[2]);
-        d.zref = finite_or_zero(z.m);
-        d.zmul = z.s == 0.0f ? 0.0f : 1.0f / z.s;
-        ln_zmul = z.s == 0.0f ? 0.0f : -kLn2 * log2_fast(z.s);
-    }
-    const float ln_s = kLn2 * log2_fast(a.s);
-    float loss = 0.0f;
-    double q = 0.0;
-    for (long long i = threadIdx.x; i < P.k; i += kDistillFinish) {
-        const long long t = columns[i];
-        if (t < 0) continue;
-        const float z = load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i)), lq = ln_share(z, d, tail, ln_zmul, P.inv_t), qi = expf(lq);
-        if (tail) q += exact_share(z, d.zref, P.inv_t);
-        if (t >= (long long)P.n) {
-            loss += __builtin_nanf("");
-        } else if (qi != 0.0f) {
-            const float x = RowElem<DT>::load(r.x, (u32)t);
-            loss += qi * (lq - (a.s == 0.0f ? -__builtin_inff() : (x - a.m) * P.inv_t - ln_s));
-        }
-    }
-    loss = sum_block<kDistillFinish>(loss, (float*)sums[0]);
-    if (tail) q = sum_block<kDistillFinish>(q, sums[1]);
-    loss += tail ? finish_row<true>(d, a, others, q, z.s, P) : finish_row<false>(d, a, others, q, z.s, P);
-    if (threadIdx.x == 0) {
-        P.loss[row] = loss;
-        if (P.rows) P.rows[row] = d;
-    }
+    if (TAIL) listed = soft_block<kDistillFinish, false>(listed, P.c, sm[1]);
+    loss_of_row<DT, TAIL, kDistillFinish>(P, row, r, a, listed, sm[2], sums);
 }
 
 constexpr int kDistillGradBlock = 256, kDistillGradVecs = 4;
@@ -159,8 +169,12 @@ __global__ void __launch_bounds__(kDistillGradBlock) k_distill_grad(DistillParam
 
 constexpr int64_t kDistillMostVecs = (int64_t)1 << 15;  // (the bitmaps: a byte each)
 
+// One workgroup per row, which then has its loss too, or several, and a launch more.
+constexpr int kPartBlock = 256;
+constexpr int64_t kFewRows = 512;
+static bool whole_rows(int64_t batch, int64_t n, int eb) { return (n + 14) * eb <= 16 * kDistillMostVecs && (batch >= 128 || n * eb <= 65536); }
 static RowParts distill_parts(int64_t batch, int64_t n, int eb) {
-    return deal_row(batch, n, eb, kDistillBlock * kDistillVecs, 2048, kDistillMostVecs);
+    return deal_row(batch, n, eb, kPartBlock * kDistillVecs, 2048, kDistillMostVecs);
 }
 
 // 16-byte vectors that a row may take: one more than its bytes need where rows do not all start on a multiple of 16.
@@ -233,12 +247,29 @@ rtopk_status rtopk_distill(const void* student, int64_t batch, int64_t n, int64_
     (void)hipGetLastError();  // an error left by earlier HIP calls of the process is not this call's
     return by_type(dt, [&](auto t) {
         constexpr int DT = decltype(t)::value;
+        if (whole_rows(batch, n, dt == RTOPK_F32 ? 4 : 2)) {
+            P.part_vecs = (u32)((n + 2 * (RowElem<DT>::E - 1)) / RowElem<DT>::E);
+            auto of = [&](auto is_tail, auto block) {
+                constexpr bool TAIL = decltype(is_tail)::value;
+                constexpr int B = decltype(block)::value;
+                for (P.row0 = 0; P.row0 < batch; P.row0 += kMostWorkgroups) {
+                    const unsigned now = (unsigned)(batch - P.row0 < kMostWorkgroups ? batch - P.row0 : kMostWorkgroups);
+                    hipLaunchKernelGGL((k_distill_part<DT, TAIL, B, true>), dim3(now), dim3(B), TAIL ? P.part_vecs + 3 : 0, st, P);
+                }
+            };
+            auto by_block = [&](auto is_tail) { batch <= kFewRows ? of(is_tail, std::integral_constant<int, 1024>{}) : of(is_tail, std::integral_constant<int, 256>{}); };
+            teacher_lse ? by_block(std::true_type{}) : by_block(std::false_type{});
+            return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
+        }
         const int64_t rows = kMostWorkgroups / d.parts > 0 ? kMostWorkgroups / d.parts : 1;
         for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
             const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
-            if (teacher_lse) hipLaunchKernelGGL((k_distill_part<DT, true>), dim3(now * d.parts), dim3(kDistillBlock), d.vecs, st, P);
-            else hipLaunchKernelGGL((k_distill_part<DT, false>), dim3(now * d.parts), dim3(kDistillBlock), 0, st, P);
-            hipLaunchKernelGGL((k_distill_finish<DT>), dim3(now), dim3(kDistillFinish), 0, st, P);
+            auto of = [&](auto is_tail) {
+                constexpr bool TAIL = decltype(is_tail)::value;
+                hipLaunchKernelGGL((k_distill_part<DT, TAIL, kPartBlock, false>), dim3(now * d.parts), dim3(kPartBlock), TAIL ? d.vecs : 0, st, P);
+                hipLaunchKernelGGL((k_distill_finish<DT, TAIL>), dim3(now), dim3(kDistillFinish), 0, st, P);
+            };
+            teacher_lse ? of(std::true_type{}) : of(std::false_type{});
         }
         return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
     });

@@ -139,12 +139,11 @@ struct RowView {
 __device__ __forceinline__ u32 part_end(u32 v0, u32 vecs, u32 nvec) { return max(v0, min(v0 + vecs, nvec)); }
 
 // f(vectors, first) for every tile of vectors [v0, v1): lane t of the workgroup holds vectors first + t, first + t + B, ...; what lies outside
-// the row or the range is -inf.
+// the row or the range is -inf.  The next tile is on its way while f has this one.
 template <int DT, int B, int V, bool NT, class F>
 __device__ __forceinline__ void sweep_vectors(const RowView<DT>& r, u32 v0, u32 v1, F&& f) {
     const u32x4 none = {RowElem<DT>::kMinusInf, RowElem<DT>::kMinusInf, RowElem<DT>::kMinusInf, RowElem<DT>::kMinusInf};
-    for (u32 t = v0; t < v1; t += B * V) {
-        u32x4 q[V];
+    auto fetch = [&](u32 t, u32x4 (&q)[V]) {
         if (t + B * V <= v1 && r.whole(t) && r.whole(t + B * V - 1)) {
 #pragma unroll
             for (int i = 0; i < V; ++i) q[i] = r.template load<NT>(t + i * B + threadIdx.x);
@@ -156,7 +155,26 @@ __device__ __forceinline__ void sweep_vectors(const RowView<DT>& r, u32 v0, u32 
                 if (v < v1) q[i] = r.trimmed(r.template load<NT>(v), v);
             }
         }
+    };
+    if (v0 >= v1) return;
+    u32x4 p[V], q[V];
+    u32 t = v0;
+    fetch(t, p);
+    for (;;) {
+        if (t + B * V >= v1) {
+            f(p, t);
+            return;
+        }
+        fetch(t + B * V, q);
+        f(p, t);
+        t += B * V;
+        if (t + B * V >= v1) {
+            f(q, t);
+            return;
+        }
+        fetch(t + B * V, p);
         f(q, t);
+        t += B * V;
     }
 }
 
