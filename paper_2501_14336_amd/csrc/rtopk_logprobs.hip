@@ -13,6 +13,8 @@ struct LogprobsParams {
     float c, inv_t;
     const long long* tokens;   // [batch][m]
     const char* top_values;    // [batch][k], in the logits' type
+    u64* part_top;             // [batch][parts][k]: the parts' best entries, best first; 0 where a part has fewer
+    long long* top_indices;
     float4* partial;           // [batch][parts]
     float *logprobs, *entropy, *top_logprobs, *row_stats;
     // the gradient
@@ -26,58 +28,356 @@ __device__ __forceinline__ float logprob_of(float x, float m, float s, float ln_
     return s == 0.0f ? -__builtin_inff() : (x - m) * inv_t - ln_s;
 }
 
-constexpr int kStatsBlock = 256, kStatsVecs = 4;
+// ------------------------------------------------------------------------------------------------
+// The k best of a sweep (k up to 64), on the way.  Elements are entries: the key of the number, NaN above all, above the complement of the column, so that all differ and the
+// larger is the better one.
+//
+// A lane keeps its running maximum for the softmax anyway.  Of W waves' lane maxima, the smallest of the waves' (k / W)-th largest has at least k elements that are not below it: a
+// bound of the k-th best.  One is taken after the first tile; from then on a lane notes the vectors whose maximum is not below it, a bit each.  Another, from
+// all the lanes have seen, is taken at the end, and only what was noted by lanes whose maximum is not below that is fetched again: of data in no order about twice k vectors, of which about
+// as many elements are listed and ranked by comparing each with all others.  A list too long for LDS (equal elements, or the best in few lanes) leads to a radix selection of the
+// part, whose cost does not depend on the data.
+// ------------------------------------------------------------------------------------------------
+constexpr int kMostTop = 64;
+constexpr u32 kListRoom = 1024;
+constexpr u32 kNotedVecs = 64;     // vectors of a lane: bits of its note
+constexpr u32 kMostEntries = 4096;  // of a row's parts together
+static_assert(kMostEntries / 256 * kMostTop <= kListRoom, "what k_logprobs_finish lists");
 
-template <int DT, bool W>
-__global__ void __launch_bounds__(kStatsBlock) k_logprobs_part(LogprobsParams P) {
-    __shared__ float4 sm[kStatsBlock / 64];
-    const u32 part = blockIdx.x % P.parts;
-    const long long row = P.row0 + blockIdx.x / P.parts;
+__device__ __forceinline__ u32 key_of(float x) { return KeyOf<RTOPK_F32>::key(__float_as_uint(x)); }
+__device__ __forceinline__ float number_of(u32 key) { return __uint_as_float((key & 0x80000000u) ? (key ^ 0x80000000u) : ~key); }  // (the key of all NaNs gives one)
+__device__ __forceinline__ u64 entry_of(u32 key, u32 col) { return ((u64)key << 32) | (u32)~col; }
+
+template <class T>
+__device__ __forceinline__ T wave_largest(T v) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const T o = __shfl_xor(v, d);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+// A bound that at least `want` of the workgroup's threads' values are not below, if there are as many values; 0 if not.  `sm` has an entry per wave and is free after the next barrier.
+template <int B, class T>
+__device__ __forceinline__ T bound_of_threads(T v, u32 want, T* sm) {
+    const u32 of_wave = (want + B / 64 - 1) / (B / 64);
+    T best = 0;
+    for (u32 i = 0; i < of_wave; ++i) {
+        best = wave_largest(v);
+        const u64 who = ballot64(v == best);
+        if (lane_id() == (u32)__builtin_ctzll(who)) v = 0;
+    }
+    if (lane_id() == 0) sm[threadIdx.x >> 6] = best;
+    __syncthreads();
+    T b = sm[threadIdx.x % (B / 64)];
+#pragma unroll
+    for (int d = 1; d < B / 64; d *= 2) {
+        const T o = __shfl_xor(b, d);
+        b = o < b ? o : b;
+    }
+    return b;
+}
+
+template <int B>
+struct TopShared {
+    u64 list[kListRoom];
+    u32 hist[256];
+    u64 bound64[B / 64];
+    u32 bound[B / 64];
+    u32 count, digit, above, scan[B / 64];
+};
+
+// list[0, count) in order to out(rank, entry), the best `want` of them.
+template <int B, class Out>
+__device__ __forceinline__ void rank_list(const u64* list, u32 count, u32 want, Out&& out) {
+    for (u32 i = threadIdx.x; i < count; i += B) {
+        const u64 e = list[i];
+        u32 rank = 0;
+        for (u32 j = 0; j < count; ++j) rank += list[j] > e;
+        if (rank < want) out(rank, e);
+    }
+}
+
+// The `want` best entries of the part's columns into sm.list, in no order; they are there after the next barrier.
+template <int DT, int B>
+__device__ __noinline__ void select_radix(const RowView<DT> r, u32 v0, u32 v1, u32 want, TopShared<B>& sm) {
+    constexpr int E = RowElem<DT>::E;
+    auto each = [&](u32 v, auto&& f) {  // f(key, column) for the elements of a vector
+        float x[E];
+        RowElem<DT>::unpack(r.template load<false>(v), x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const u32 col = v * E + j - r.lead;
+            if (col < r.n) f(key_of(x[j]), col);
+        }
+    };
+    u32 prefix = 0, rank = want;  // the key's digits so far; its rank among those that have them
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        __syncthreads();
+        for (u32 i = threadIdx.x; i < 256; i += B) sm.hist[i] = 0;
+        __syncthreads();
+        for (u32 v = v0 + threadIdx.x; v < v1; v += B)
+            each(v, [&](u32 key, u32) {
+                if (shift == 24 || (key >> ((shift + 8) & 31)) == prefix) {
+                    const u32 digit = (key >> shift) & 255u, first = __builtin_amdgcn_readfirstlane(digit);
+                    const u64 alike = ballot64(digit == first), all = ballot64(true);
+                    if (alike == all) {  // (a crowd: one add for the wave)
+                        if (lane_id() == (u32)__builtin_ctzll(all)) atomicAdd(&sm.hist[first], (u32)__builtin_popcountll(all));
+                    } else {
+                        atomicAdd(&sm.hist[digit], 1u);
+                    }
+                }
+            });
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            u32 d = 255, above = 0;
+            while (d > 0 && above + sm.hist[d] < rank) above += sm.hist[d--];
+            sm.digit = d;
+            sm.above = above;
+        }
+        __syncthreads();
+        rank -= sm.above;
+        prefix = (prefix << 8) | sm.digit;
+    }
+    // what is better, and the first `rank` of what is equal
+    if (threadIdx.x == 0) sm.count = 0;
+    __syncthreads();
+    for (u32 v = v0 + threadIdx.x; v < v1; v += B)
+        each(v, [&](u32 key, u32 col) {
+            if (key > prefix) sm.list[atomicAdd(&sm.count, 1u)] = entry_of(key, col);
+        });
+    __syncthreads();
+    u32 found = 0;
+    for (u32 t = v0; t < v1 && found < rank; t += B) {
+        const u32 v = t + threadIdx.x;
+        u32 mine = 0;
+        if (v < v1) each(v, [&](u32 key, u32) { mine += key == prefix; });
+        u32 before = mine;  // inclusive sums over the wave, then over the waves
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const u32 o = (u32)__shfl_up((int)before, d);
+            before += lane_id() >= (u32)d ? o : 0u;
+        }
+        if (lane_id() == 63) sm.scan[threadIdx.x >> 6] = before;
+        __syncthreads();
+        u32 total = 0;
+        for (u32 w = 0; w < B / 64; ++w) {
+            if (w == threadIdx.x >> 6) before += total;
+            total += sm.scan[w];
+        }
+        u32 at = found + before - mine;
+        if (v < v1)
+            each(v, [&](u32 key, u32 col) {
+                if (key == prefix && at++ < rank) sm.list[want - rank + at - 1] = entry_of(key, col);
+            });
+        found += total;
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// The sweep of a row or a part of one.
+// ------------------------------------------------------------------------------------------------
+template <int DT>
+__device__ __forceinline__ void write_logprob(const LogprobsParams& P, long long row, long long i, float x, long long t, const SoftSum& a, float ln_s) {
+    float v = 0.0f;
+    if (t >= (long long)P.n) v = __builtin_nanf("");
+    else if (t >= 0) v = logprob_of(x, a.m, a.s, ln_s, P.inv_t);
+    P.logprobs[row * P.m + i] = v;
+}
+template <bool W>
+__device__ __forceinline__ void write_stats(const LogprobsParams& P, long long row, const SoftSum& a, float ln_s) {
+    if (W) P.entropy[row] = a.s == 0.0f ? 0.0f : ln_s - kLn2 * (a.w / a.s);
+    if (P.row_stats) {
+        P.row_stats[2 * row] = a.m;
+        P.row_stats[2 * row + 1] = a.s;
+    }
+}
+__device__ __forceinline__ void write_top(const LogprobsParams& P, long long row, u32 rank, u64 e, const SoftSum& a, float ln_s) {
+    P.top_logprobs[row * P.k + rank] = logprob_of(number_of((u32)(e >> 32)), a.m, a.s, ln_s, P.inv_t);
+    P.top_indices[row * P.k + rank] = (long long)(u32)~(u32)e;
+}
+
+struct NoTop {};
+
+template <int DT, int B, int V, bool W, bool TOP, bool WHOLE>
+__global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
+    constexpr int E = RowElem<DT>::E;
+    __shared__ float4 sm[B / 64];
+    __shared__ std::conditional_t<TOP, TopShared<B>, NoTop> top;
+    const u32 part = WHOLE ? 0u : blockIdx.x % P.parts;
+    const long long row = P.row0 + (WHOLE ? blockIdx.x : blockIdx.x / P.parts);
     const RowView<DT> r(P.logits, row, P.row_bytes, P.n);
     const u32 v0 = part * P.part_vecs, v1 = part_end(v0, P.part_vecs, r.nvec);
+    const bool one_tile = v1 - v0 <= B * V;  // what is listed is listed from the registers
+    long long token = -1;  // the thread's first
+    float x_of = 0.0f;
+    if (WHOLE && (long long)threadIdx.x < P.m) {
+        token = P.tokens[row * P.m + threadIdx.x];
+        if (token >= 0 && token < (long long)P.n) x_of = RowElem<DT>::load(r.x, (u32)token);
+    }
     SoftSum a;
-    sweep_vectors<DT, kStatsBlock, kStatsVecs, false>(r, v0, v1, [&](const u32x4 (&q)[kStatsVecs], u32) {
-        constexpr int E = RowElem<DT>::E;
-        float x[kStatsVecs * E];
+    u64 noted = 0;
+    u32 bound = 0, tiles = 0;
+    float bound_number = -__builtin_inff();
+    if constexpr (TOP) {
+        if (threadIdx.x == 0) top.count = 0;
+    }
+    auto list_vector = [&](u32 v, const float (&x)[E]) {
+        if constexpr (TOP) {
 #pragma unroll
-        for (int i = 0; i < kStatsVecs; ++i) {
+            for (int j = 0; j < E; ++j) {
+                const u32 col = v * E + j - r.lead;
+                if (!(x[j] < bound_number) && col < r.n && key_of(x[j]) >= bound) {
+                    const u32 place = atomicAdd(&top.count, 1u);
+                    if (place < kListRoom) top.list[place] = entry_of(key_of(x[j]), col);
+                }
+            }
+        }
+    };
+    sweep_vectors<DT, B, V, false>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
+        float x[V * E], most[V], t = a.m;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
             float y[E];
             RowElem<DT>::unpack(q[i], y);
+            most[i] = largest(-__builtin_inff(), y);
+            t = __builtin_elementwise_maximum(t, most[i]);
 #pragma unroll
             for (int j = 0; j < E; ++j) x[i * E + j] = y[j];
         }
-        soft_add<W>(a, x, P.c);
+        soft_add_to<W>(a, x, t, P.c);
+        if constexpr (TOP) {
+            if (first == v0) {
+                bound = bound_of_threads<B>(first + threadIdx.x < v1 ? key_of(a.m) : 0u, (u32)P.k, top.bound);
+                bound_number = bound == 0 ? -__builtin_inff() : number_of(bound);
+            }
+            u32 hits = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) hits |= !(most[i] < bound_number) ? 1u << i : 0u;
+            if (one_tile) {
+                if (hits) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float y[E];
+#pragma unroll
+                        for (int j = 0; j < E; ++j) y[j] = x[i * E + j];
+                        if ((hits >> i) & 1) list_vector(first + i * B + threadIdx.x, y);
+                    }
+                }
+            } else {
+                noted |= (u64)hits << (tiles * V);
+                ++tiles;
+            }
+        }
     });
-    a = soft_block<kStatsBlock, W>(a, P.c, sm);
-    if (threadIdx.x == 0) P.partial[row * P.parts + part] = packed(a);
+    const float mine = a.m;
+    a = soft_block<B, W>(a, P.c, sm);
+    const float ln_s = kLn2 * log2_fast(a.s);
+    if constexpr (TOP) {
+        const long long here = (long long)min((u64)v1 * E, (u64)r.lead + r.n) - (long long)max((u64)v0 * E, (u64)r.lead);  // columns
+        const u32 want = here < P.k ? (here < 0 ? 0u : (u32)here) : (u32)P.k;
+        if (!one_tile) {
+            bound = max(bound, bound_of_threads<B>(key_of(mine), (u32)P.k, (u32*)top.bound64));
+            bound_number = bound == 0 ? -__builtin_inff() : number_of(bound);
+            if (!(mine < bound_number)) {
+                while (noted) {
+                    // (four vectors on their way at a time)
+                    u32 at[4];
+                    u32x4 q[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        at[i] = noted ? v0 + (u32)__builtin_ctzll(noted) * B + threadIdx.x : v1;
+                        noted &= noted - 1;
+                        if (at[i] < v1) q[i] = r.template load<false>(at[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (at[i] < v1) {
+                            float x[E];
+                            RowElem<DT>::unpack(q[i], x);
+                            list_vector(at[i], x);
+                        }
+                }
+            }
+        }
+        __syncthreads();
+        u32 count = top.count;
+        if (count > kListRoom || count < want) {
+            select_radix<DT, B>(r, v0, v1, want, top);
+            __syncthreads();
+            count = want;
+        }
+        if (WHOLE) {
+            rank_list<B>(top.list, count, want, [&](u32 rank, u64 e) { write_top(P, row, rank, e, a, ln_s); });
+        } else {
+            u64* out = P.part_top + (row * P.parts + part) * P.k;
+            rank_list<B>(top.list, count, want, [&](u32 rank, u64 e) { out[rank] = e; });
+            for (u32 i = want + threadIdx.x; i < (u32)P.k; i += B) out[i] = 0;
+        }
+    }
+    if (!WHOLE) {
+        if (threadIdx.x == 0) P.partial[row * P.parts + part] = packed(a);
+        return;
+    }
+    if (!TOP)
+        for (long long i = threadIdx.x; i < P.k; i += B)
+            P.top_logprobs[row * P.k + i] = logprob_of(RowElem<DT>::load(P.top_values + (size_t)(row * P.k) * RowElem<DT>::kBytes, (u32)i), a.m, a.s, ln_s, P.inv_t);
+    for (long long i = threadIdx.x; i < P.m; i += B) {
+        if (i >= B) {
+            token = P.tokens[row * P.m + i];
+            x_of = token >= 0 && token < (long long)P.n ? RowElem<DT>::load(r.x, (u32)token) : 0.0f;
+        }
+        write_logprob<DT>(P, row, i, x_of, token, a, ln_s);
+    }
+    if (threadIdx.x == 0) write_stats<W>(P, row, a, ln_s);
 }
 
-constexpr int kFinishBlock = 64;
+// A row's parts put together.  TOP: their lists too; otherwise the alternatives' values are there already (P.top_values).
+constexpr int kFinishBlock = 256;
 
-template <int DT, bool W>
+template <int DT, bool W, bool TOP>
 __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams P) {
+    __shared__ float4 sm[kFinishBlock / 64];
+    __shared__ std::conditional_t<TOP, TopShared<kFinishBlock>, NoTop> top;
     const long long row = P.row0 + blockIdx.x;
     const RowView<DT> r(P.logits, row, P.row_bytes, P.n);
     SoftSum a;
     for (u32 i = threadIdx.x; i < P.parts; i += kFinishBlock) a = soft_join<W>(a, unpacked(P.partial[row * P.parts + i]), P.c);
-    a = soft_block<kFinishBlock, W>(a, P.c, nullptr);
+    u64 best = 0;
+    const u64* lists = P.part_top + row * P.parts * P.k;
+    const u32 entries = TOP ? P.parts * (u32)P.k : 0u;
+    for (u32 i = threadIdx.x; i < entries; i += kFinishBlock) best = max(best, lists[i]);
+    a = soft_block<kFinishBlock, W>(a, P.c, sm);
     const float ln_s = kLn2 * log2_fast(a.s);
+    if constexpr (TOP) {
+        if (threadIdx.x == 0) top.count = 0;
+        // the k-th best of the threads' best ones: k threads have any that are not below it, and at most kMostEntries / 256 each, which the list has room for
+        top.list[threadIdx.x] = best;
+        __syncthreads();
+        u32 rank = 0;
+        for (u32 j = 0; j < kFinishBlock; ++j) rank += top.list[j] > best || (top.list[j] == best && j < threadIdx.x);
+        if (rank == (u32)P.k - 1) top.bound64[0] = best;
+        __syncthreads();
+        const u64 bound = top.bound64[0];
+        for (u32 i = threadIdx.x; i < entries; i += kFinishBlock) {
+            const u64 e = lists[i];
+            if (e >= bound && e != 0) {
+                const u32 place = atomicAdd(&top.count, 1u);
+                if (place < kListRoom) top.list[place] = e;
+            }
+        }
+        __syncthreads();
+        rank_list<kFinishBlock>(top.list, min(top.count, kListRoom), (u32)P.k, [&](u32 rank, u64 e) { write_top(P, row, rank, e, a, ln_s); });
+    } else {
+        for (long long i = threadIdx.x; i < P.k; i += kFinishBlock)
+            P.top_logprobs[row * P.k + i] = logprob_of(RowElem<DT>::load(P.top_values + (size_t)(row * P.k) * RowElem<DT>::kBytes, (u32)i), a.m, a.s, ln_s, P.inv_t);
+    }
     for (long long i = threadIdx.x; i < P.m; i += kFinishBlock) {
         const long long t = P.tokens[row * P.m + i];
-        float v = 0.0f;
-        if (t >= (long long)P.n) v = __builtin_nanf("");
-        else if (t >= 0) v = logprob_of(RowElem<DT>::load(r.x, (u32)t), a.m, a.s, ln_s, P.inv_t);
-        P.logprobs[row * P.m + i] = v;
+        write_logprob<DT>(P, row, i, t >= 0 && t < (long long)P.n ? RowElem<DT>::load(r.x, (u32)t) : 0.0f, t, a, ln_s);
     }
-    for (long long i = threadIdx.x; i < P.k; i += kFinishBlock)
-        P.top_logprobs[row * P.k + i] = logprob_of(RowElem<DT>::load(P.top_values + (size_t)(row * P.k) * RowElem<DT>::kBytes, (u32)i), a.m, a.s, ln_s, P.inv_t);
-    if (threadIdx.x == 0) {
-        if (W) P.entropy[row] = a.s == 0.0f ? 0.0f : ln_s - kLn2 * (a.w / a.s);
-        if (P.row_stats) {
-            P.row_stats[2 * row] = a.m;
-            P.row_stats[2 * row + 1] = a.s;
-        }
-    }
+    if (threadIdx.x == 0) write_stats<W>(P, row, a, ln_s);
 }
 
 // dx_j = (1/T) [ sum_i g_i (1[t_i = j] - p_j) - gH p_j (ln p_j + H) ]
@@ -126,10 +426,67 @@ __global__ void __launch_bounds__(kGradBlock) k_logprobs_grad(LogprobsParams P) 
 
 constexpr int64_t kLogprobsMostVecs = (int64_t)1 << 15;  // (the gradient's bitmap: a byte each)
 
-static RowParts stats_parts(int64_t batch, int64_t n, int eb) {
-    return deal_row(batch, n, eb, kStatsBlock * kStatsVecs, 2048, (int64_t)1 << 28);
+// How a call goes.
+struct LogprobsPlan {
+    bool top;    // alternatives by the sweep itself (otherwise rtopk_select finds them first)
+    int block;   // a workgroup of so many threads takes a row; 0: several share one, and a second launch puts their parts together
+    u32 parts, part_vecs;
+    size_t partial_bytes, top_bytes, select_bytes;
+    size_t bytes() const { return partial_bytes + top_bytes + select_bytes; }
+};
+constexpr int kPartBlock = 256, kPartVecs = 2, kWholeVecs = 4;
+
+static rtopk_status make_plan(int64_t batch, int64_t n, int64_t m, int64_t k, rtopk_dtype dt, LogprobsPlan* L) {
+    if (batch < 1 || batch > 0x7fffffff || n < 1 || n > RTOPK_MAX_N || m < 0 || m > 0x7fffffff || k < 0 || k > n) return RTOPK_ERR_INVALID_ARG;
+    if (dt != RTOPK_F32 && dt != RTOPK_F16 && dt != RTOPK_BF16) return RTOPK_ERR_INVALID_ARG;
+    const int eb = dt == RTOPK_F32 ? 4 : 2, E = 16 / eb;
+    const int64_t vecs = (n + 2 * (E - 1)) / E;  // (wherever a row starts)
+    *L = LogprobsPlan{};
+    L->top = k > 0 && k <= kMostTop;
+    if ((batch >= 128 && vecs <= (int64_t)kNotedVecs * 1024) || vecs <= 4096) {
+        L->block = batch > 768 && vecs <= (int64_t)kNotedVecs * 256 ? 256 : batch > 384 && vecs <= (int64_t)kNotedVecs * 512 ? 512 : 1024;
+        L->parts = 1;
+        L->part_vecs = (u32)vecs;
+    } else {
+        const int64_t tile = kPartBlock * kPartVecs, most = L->top ? kMostEntries / k : (int64_t)1 << 20;
+        int64_t want = 1024 / batch < 1 ? 1 : 1024 / batch;
+        if (want > most) want = most;
+        const int64_t longest = L->top ? (int64_t)kNotedVecs * kPartBlock : (int64_t)1 << 28;
+        RowParts d = deal_row(batch, n, eb, tile, want * batch, longest);
+        if (d.parts > most) {  // a row too long for so many parts: its alternatives are selected apart
+            L->top = false;
+            d = deal_row(batch, n, eb, tile, 1024, (int64_t)1 << 28);
+        }
+        L->parts = d.parts;
+        L->part_vecs = d.vecs;
+        L->partial_bytes = up256((size_t)batch * d.parts * sizeof(float4));
+        if (L->top) L->top_bytes = up256((size_t)batch * d.parts * k * 8);
+    }
+    if (k > 0 && !L->top) {
+        size_t all = 0, one = 0;  // (rows that do not follow one another are selected from one by one)
+        const rtopk_status s = rtopk_workspace_bytes(batch, n, k, dt, RTOPK_FLAG_SORTED, &all);
+        if (s != RTOPK_OK) return s;
+        (void)rtopk_workspace_bytes(1, n, k, dt, RTOPK_FLAG_SORTED, &one);
+        L->top_bytes = up256((size_t)batch * k * eb);
+        L->select_bytes = all > one ? all : one;
+    }
+    return RTOPK_OK;
 }
-static size_t partial_bytes(int64_t batch, int64_t n, int eb) { return up256((size_t)batch * stats_parts(batch, n, eb).parts * sizeof(float4)); }
+
+template <int DT, bool W, bool TOP>
+static void launch_logprobs(LogprobsParams P, const LogprobsPlan& L, int64_t batch, hipStream_t st) {
+    const int64_t rows = kMostWorkgroups / L.parts > 0 ? kMostWorkgroups / L.parts : 1;
+    for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
+        const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
+        if (L.block == 256) hipLaunchKernelGGL((k_logprobs_sweep<DT, 256, kWholeVecs, W, TOP, true>), dim3(now), dim3(256), 0, st, P);
+        else if (L.block == 512) hipLaunchKernelGGL((k_logprobs_sweep<DT, 512, kWholeVecs, W, TOP, true>), dim3(now), dim3(512), 0, st, P);
+        else if (L.block == 1024) hipLaunchKernelGGL((k_logprobs_sweep<DT, 1024, kWholeVecs, W, TOP, true>), dim3(now), dim3(1024), 0, st, P);
+        else {
+            hipLaunchKernelGGL((k_logprobs_sweep<DT, kPartBlock, kPartVecs, W, TOP, false>), dim3(now * L.parts), dim3(kPartBlock), 0, st, P);
+            hipLaunchKernelGGL((k_logprobs_finish<DT, W, TOP>), dim3(now), dim3(kFinishBlock), 0, st, P);
+        }
+    }
+}
 
 }  // namespace rtopk
 
@@ -138,20 +495,11 @@ using namespace rtopk;
 extern "C" {
 
 rtopk_status rtopk_logprobs_workspace_bytes(int64_t batch, int64_t n, int64_t m, int64_t k, rtopk_dtype dt, size_t* bytes_out) {
-    if (!bytes_out || batch < 1 || batch > 0x7fffffff || n < 1 || n > RTOPK_MAX_N || m < 0 || k < 0 || k > n) return RTOPK_ERR_INVALID_ARG;
-    if (dt != RTOPK_F32 && dt != RTOPK_F16 && dt != RTOPK_BF16) return RTOPK_ERR_INVALID_ARG;
-    const int eb = dt == RTOPK_F32 ? 4 : 2;
-    size_t select = 0;
-    if (k > 0) {
-        const rtopk_status s = rtopk_workspace_bytes(batch, n, k, dt, RTOPK_FLAG_SORTED, &select);
-        if (s != RTOPK_OK) return s;
-        size_t one = 0;  // (rows that do not follow one another are selected from one by one)
-        (void)rtopk_workspace_bytes(1, n, k, dt, RTOPK_FLAG_SORTED, &one);
-        if (one > select) select = one;
-        select += up256((size_t)batch * k * eb);
-    }
-    *bytes_out = partial_bytes(batch, n, eb) + select;
-    return RTOPK_OK;
+    if (!bytes_out) return RTOPK_ERR_INVALID_ARG;
+    LogprobsPlan L;
+    const rtopk_status s = make_plan(batch, n, m, k, dt, &L);
+    if (s == RTOPK_OK) *bytes_out = L.bytes() > 256 ? L.bytes() : 256;
+    return s;
 }
 
 rtopk_status rtopk_logprobs(const void* logits, int64_t batch, int64_t n, int64_t row_stride, rtopk_dtype dt, float inv_temperature,
@@ -159,62 +507,53 @@ rtopk_status rtopk_logprobs(const void* logits, int64_t batch, int64_t n, int64_
                             float* out_top_logprobs, int64_t* out_top_indices, void* workspace, size_t workspace_bytes, void* hip_stream) {
     rtopk_status s = check_rows(logits, batch, n, row_stride, dt);
     if (s != RTOPK_OK) return s;
-    if (!usable_temperature(inv_temperature) || m < 0 || m > 0x7fffffff || k < 0 || k > n || !workspace) return RTOPK_ERR_INVALID_ARG;
+    if (!usable_temperature(inv_temperature) || !workspace) return RTOPK_ERR_INVALID_ARG;
+    LogprobsPlan L;
+    s = make_plan(batch, n, m, k, dt, &L);
+    if (s != RTOPK_OK) return s;
     if (m > 0 && (!tokens || !out_logprobs)) return RTOPK_ERR_INVALID_ARG;
     if (k > 0 && (!out_top_logprobs || !out_top_indices)) return RTOPK_ERR_INVALID_ARG;
     if (((uintptr_t)tokens | (uintptr_t)out_top_indices) % 8 || ((uintptr_t)out_logprobs | (uintptr_t)out_entropy | (uintptr_t)out_row_stats | (uintptr_t)out_top_logprobs) % 4 ||
         (uintptr_t)workspace % 256)
         return RTOPK_ERR_UNSUPPORTED;
-    size_t need = 0;
-    s = rtopk_logprobs_workspace_bytes(batch, n, m, k, dt, &need);
-    if (s != RTOPK_OK) return s;
-    if (workspace_bytes < need) return RTOPK_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < L.bytes() || workspace_bytes < 256) return RTOPK_ERR_WORKSPACE_TOO_SMALL;
     const int eb = dt == RTOPK_F32 ? 4 : 2;
-    const hipStream_t st = (hipStream_t)hip_stream;
     char* ws = (char*)workspace;
-    char* top_values = ws + partial_bytes(batch, n, eb);
-    if (k > 0) {
-        char* select = top_values + up256((size_t)batch * k * eb);
-        // rows that do not follow one another are selected from one by one
+    char* top = ws + L.partial_bytes;
+    if (L.select_bytes) {
+        // (rows that do not follow one another one by one)
         const int64_t at_once = batch == 1 || row_stride == n ? batch : 1;
         for (int64_t row = 0; row < batch; row += at_once) {
-            s = rtopk_select((const char*)logits + row * row_stride * eb, at_once, n, k, dt, 1, RTOPK_FLAG_SORTED, 0, top_values + row * k * eb,
-                             out_top_indices + row * k, select, workspace_bytes - (size_t)(select - ws), hip_stream);
+            s = rtopk_select((const char*)logits + row * row_stride * eb, at_once, n, k, dt, 1, RTOPK_FLAG_SORTED, 0, top + row * k * eb,
+                             out_top_indices + row * k, top + L.top_bytes, L.select_bytes, hip_stream);
             if (s != RTOPK_OK) return s;
         }
     }
-    const RowParts d = stats_parts(batch, n, eb);
     LogprobsParams P = {};
     P.logits = (const char*)logits;
     P.row_bytes = row_stride * eb;
     P.n = (u32)n;
     P.m = m;
     P.k = k;
-    P.parts = d.parts;
-    P.part_vecs = d.vecs;
+    P.parts = L.parts;
+    P.part_vecs = L.part_vecs;
     P.c = inv_temperature * kLog2e;
     P.inv_t = inv_temperature;
     P.tokens = (const long long*)tokens;
-    P.top_values = top_values;
+    P.top_values = top;
+    P.part_top = (u64*)top;
+    P.top_indices = (long long*)out_top_indices;
     P.partial = (float4*)ws;
     P.logprobs = out_logprobs;
     P.entropy = out_entropy;
     P.top_logprobs = out_top_logprobs;
     P.row_stats = out_row_stats;
+    const hipStream_t st = (hipStream_t)hip_stream;
     (void)hipGetLastError();  // an error left by earlier HIP calls of the process is not this call's
     return by_type(dt, [&](auto t) {
         constexpr int DT = decltype(t)::value;
-        const int64_t rows = kMostWorkgroups / d.parts > 0 ? kMostWorkgroups / d.parts : 1;
-        for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
-            const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
-            if (out_entropy) {
-                hipLaunchKernelGGL((k_logprobs_part<DT, true>), dim3(now * d.parts), dim3(kStatsBlock), 0, st, P);
-                hipLaunchKernelGGL((k_logprobs_finish<DT, true>), dim3(now), dim3(kFinishBlock), 0, st, P);
-            } else {
-                hipLaunchKernelGGL((k_logprobs_part<DT, false>), dim3(now * d.parts), dim3(kStatsBlock), 0, st, P);
-                hipLaunchKernelGGL((k_logprobs_finish<DT, false>), dim3(now), dim3(kFinishBlock), 0, st, P);
-            }
-        }
+        if (out_entropy) L.top ? launch_logprobs<DT, true, true>(P, L, batch, st) : launch_logprobs<DT, true, false>(P, L, batch, st);
+        else L.top ? launch_logprobs<DT, false, true>(P, L, batch, st) : launch_logprobs<DT, false, false>(P, L, batch, st);
         return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
     });
 }

@@ -210,18 +210,25 @@ __device__ __forceinline__ float largest(float t, const float (&x)[N]) {
     for (int j = 0; j < N; ++j) t = __builtin_elementwise_maximum(t, x[j]);
     return t;
 }
+// N numbers, of which none is above t, and t not below a's maximum.
 template <bool W, int N>
-__device__ __forceinline__ void soft_add(SoftSum& a, const float (&x)[N], float c) {
-    const float t = largest(a.m, x), ref = finite_or_zero(t);
+__device__ __forceinline__ void soft_add_to(SoftSum& a, const float (&x)[N], float t, float c) {
+    const float ref = finite_or_zero(t);
     soft_rescale<W>(a, t, ref, c);
-    // The exponent in one fused step, x c - r with r the rounded ref c; the sum is put right for what that rounding took off.  (Not where ref c leaves the range: logits at a type's lowest
+    // The exponent in one fused step, x c - r with r the rounded ref c; the sums are put right for what that rounding took off.  (Not where ref c leaves the range: logits at a type's lowest
     // or highest values.)
     const float r = ref * c, off = __builtin_fmaf(ref, c, -r);
-    if (!W && ballot64(!(fabsf(r) < 1e30f)) == 0) {
-        float s = 0.0f;
+    if (ballot64(!(fabsf(r) < 1e30f)) == 0) {
+        float s = 0.0f, w = 0.0f;
 #pragma unroll
-        for (int j = 0; j < N; ++j) s += exp2_fast(__builtin_fmaf(x[j], c, -r));
-        a.s += s * exp2_fast(-off);
+        for (int j = 0; j < N; ++j) {
+            const float y = __builtin_fmaf(x[j], c, -r), e = exp2_fast(y);
+            s += e;
+            if (W) w = __builtin_fmaf(e, fmaxf(y, kNothing), w);
+        }
+        const float f = exp2_fast(-off);
+        if (W) a.w += f * (w - off * s);
+        a.s += s * f;
         return;
     }
 #pragma unroll
@@ -231,6 +238,8 @@ __device__ __forceinline__ void soft_add(SoftSum& a, const float (&x)[N], float 
         if (W) a.w += e * fmaxf(y, kNothing);
     }
 }
+template <bool W, int N>
+__device__ __forceinline__ void soft_add(SoftSum& a, const float (&x)[N], float c) { soft_add_to<W>(a, x, largest(a.m, x), c); }
 template <bool W>
 __device__ __forceinline__ SoftSum soft_join(SoftSum a, SoftSum b, float c) {
     const float m = __builtin_elementwise_maximum(a.m, b.m), ref = finite_or_zero(m);
@@ -254,26 +263,37 @@ __device__ __forceinline__ SoftSum soft_wave(SoftSum a, float c) {
     return a;
 }
 // Over the workgroup, the same in every thread.  `sm` has an entry per wave; it may be used again after the next barrier.  (Waves' sums are joined across lanes: read by every lane,
-// those of 16 waves would take 64 registers.)
+// those of 16 waves would take 64 registers.  Lanes of a pair may round differently, with a product and a sum fused on one side: all take the first lane's.)
+__device__ __forceinline__ SoftSum uniform(const SoftSum& a) {
+    SoftSum b;
+    b.m = uniform(a.m);
+    b.s = uniform(a.s);
+    b.w = uniform(a.w);
+    return b;
+}
+__device__ __forceinline__ double uniform(double x) {
+    const u64 v = __builtin_bit_cast(u64, x);
+    return __builtin_bit_cast(double, ((u64)(u32)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (u32)__builtin_amdgcn_readfirstlane((int)(u32)v));
+}
 template <int B, bool W>
 __device__ __forceinline__ SoftSum soft_block(SoftSum a, float c, float4* sm) {
     a = soft_wave<W>(a, c);
-    if constexpr (B == 64) return a;
+    if constexpr (B == 64) return uniform(a);
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = packed(a);
     __syncthreads();
-    return soft_wave<W, B / 64>(unpacked(sm[threadIdx.x % (B / 64)]), c);
+    return uniform(soft_wave<W, B / 64>(unpacked(sm[threadIdx.x % (B / 64)]), c));
 }
 template <int B, class T>
 __device__ __forceinline__ T sum_block(T v, T* sm) {  // likewise
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    if constexpr (B == 64) return v;
+    if constexpr (B == 64) return uniform(v);
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
     __syncthreads();
     v = sm[threadIdx.x % (B / 64)];
 #pragma unroll
     for (int d = 1; d < B / 64; d *= 2) v += __shfl_xor(v, d);
-    return v;
+    return uniform(v);
 }
 
 // ------------------------------------------------------------------------------------------------
