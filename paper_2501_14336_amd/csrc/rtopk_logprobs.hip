@@ -48,15 +48,6 @@ __device__ __forceinline__ u32 key_of(float x) { return KeyOf<RTOPK_F32>::key(__
 __device__ __forceinline__ float number_of(u32 key) { return __uint_as_float((key & 0x80000000u) ? (key ^ 0x80000000u) : ~key); }  // (the key of all NaNs gives one)
 __device__ __forceinline__ u64 entry_of(u32 key, u32 col) { return ((u64)key << 32) | (u32)~col; }
 
-template <class T>
-__device__ __forceinline__ T wave_largest(T v) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const T o = __shfl_xor(v, d);
-        v = o > v ? o : v;
-    }
-    return v;
-}
 // A bound that at least `want` of the workgroup's threads' values are not below, if there are as many values; 0 if not.  `sm` has an entry per wave and is free after the next barrier.
 template <int B, class T>
 __device__ __forceinline__ T bound_of_threads(T v, u32 want, T* sm) {
@@ -69,13 +60,7 @@ __device__ __forceinline__ T bound_of_threads(T v, u32 want, T* sm) {
     }
     if (lane_id() == 0) sm[threadIdx.x >> 6] = best;
     __syncthreads();
-    T b = sm[threadIdx.x % (B / 64)];
-#pragma unroll
-    for (int d = 1; d < B / 64; d *= 2) {
-        const T o = __shfl_xor(b, d);
-        b = o < b ? o : b;
-    }
-    return b;
+    return wave_smallest(sm[lane_id() % (B / 64)]);
 }
 
 template <int B>
@@ -93,6 +78,7 @@ __device__ __forceinline__ void rank_list(const u64* list, u32 count, u32 want, 
     for (u32 i = threadIdx.x; i < count; i += B) {
         const u64 e = list[i];
         u32 rank = 0;
+#pragma unroll 8  // (a trip to LDS for eight at a time)
         for (u32 j = 0; j < count; ++j) rank += list[j] > e;
         if (rank < want) out(rank, e);
     }
@@ -342,40 +328,54 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
     __shared__ std::conditional_t<TOP, TopShared<kFinishBlock>, NoTop> top;
     const long long row = P.row0 + blockIdx.x;
     const RowView<DT> r(P.logits, row, P.row_bytes, P.n);
-    SoftSum a;
-    for (u32 i = threadIdx.x; i < P.parts; i += kFinishBlock) a = soft_join<W>(a, unpacked(P.partial[row * P.parts + i]), P.c);
-    u64 best = 0;
+    // everything that has to be fetched at once: what other compute units wrote is far away
+    long long token = -1;  // the thread's first
+    if ((long long)threadIdx.x < P.m) token = P.tokens[row * P.m + threadIdx.x];
     const u64* lists = P.part_top + row * P.parts * P.k;
     const u32 entries = TOP ? P.parts * (u32)P.k : 0u;
-    for (u32 i = threadIdx.x; i < entries; i += kFinishBlock) best = max(best, lists[i]);
+    constexpr int kEach = TOP ? kMostEntries / kFinishBlock : 1;
+    u64 e[kEach], best = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const u32 i = j * kFinishBlock + threadIdx.x;
+        e[j] = i < entries ? lists[i] : 0;
+    }
+    SoftSum a;
+    for (u32 i = threadIdx.x; i < P.parts; i += kFinishBlock) a = soft_join<W>(a, unpacked(P.partial[row * P.parts + i]), P.c);
+    float x_of = token >= 0 && token < (long long)P.n ? RowElem<DT>::load(r.x, (u32)token) : 0.0f;
     a = soft_block<kFinishBlock, W>(a, P.c, sm);
     const float ln_s = kLn2 * log2_fast(a.s);
     if constexpr (TOP) {
         if (threadIdx.x == 0) top.count = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) best = max(best, e[j]);
         // the k-th best of the threads' best ones: k threads have any that are not below it, and at most kMostEntries / 256 each, which the list has room for
         top.list[threadIdx.x] = best;
         __syncthreads();
         u32 rank = 0;
+#pragma unroll 16
         for (u32 j = 0; j < kFinishBlock; ++j) rank += top.list[j] > best || (top.list[j] == best && j < threadIdx.x);
         if (rank == (u32)P.k - 1) top.bound64[0] = best;
         __syncthreads();
         const u64 bound = top.bound64[0];
-        for (u32 i = threadIdx.x; i < entries; i += kFinishBlock) {
-            const u64 e = lists[i];
-            if (e >= bound && e != 0) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (e[j] >= bound && e[j] != 0) {
                 const u32 place = atomicAdd(&top.count, 1u);
-                if (place < kListRoom) top.list[place] = e;
+                if (place < kListRoom) top.list[place] = e[j];
             }
-        }
         __syncthreads();
-        rank_list<kFinishBlock>(top.list, min(top.count, kListRoom), (u32)P.k, [&](u32 rank, u64 e) { write_top(P, row, rank, e, a, ln_s); });
+        rank_list<kFinishBlock>(top.list, min(top.count, kListRoom), (u32)P.k, [&](u32 rank, u64 x) { write_top(P, row, rank, x, a, ln_s); });
     } else {
         for (long long i = threadIdx.x; i < P.k; i += kFinishBlock)
             P.top_logprobs[row * P.k + i] = logprob_of(RowElem<DT>::load(P.top_values + (size_t)(row * P.k) * RowElem<DT>::kBytes, (u32)i), a.m, a.s, ln_s, P.inv_t);
     }
     for (long long i = threadIdx.x; i < P.m; i += kFinishBlock) {
-        const long long t = P.tokens[row * P.m + i];
-        write_logprob<DT>(P, row, i, t >= 0 && t < (long long)P.n ? RowElem<DT>::load(r.x, (u32)t) : 0.0f, t, a, ln_s);
+        if (i >= kFinishBlock) {
+            token = P.tokens[row * P.m + i];
+            x_of = token >= 0 && token < (long long)P.n ? RowElem<DT>::load(r.x, (u32)token) : 0.0f;
+        }
+        write_logprob<DT>(P, row, i, x_of, token, a, ln_s);
     }
     if (threadIdx.x == 0) write_stats<W>(P, row, a, ln_s);
 }

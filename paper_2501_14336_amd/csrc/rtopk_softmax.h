@@ -249,51 +249,74 @@ __device__ __forceinline__ SoftSum soft_join(SoftSum a, SoftSum b, float c) {
     if (W) a.w += b.w;
     return a;
 }
-// Over LANES lanes that follow one another, the same in all of them.
-template <bool W, int LANES = 64>
-__device__ __forceinline__ SoftSum soft_wave(SoftSum a, float c) {
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) {
-        SoftSum b;
-        b.m = __shfl_xor(a.m, d);
-        b.s = __shfl_xor(a.s, d);
-        if (W) b.w = __shfl_xor(a.w, d);
-        a = soft_join<W>(a, b, c);
+// ------------------------------------------------------------------------------------------------
+// Over a wave and over a workgroup; results are the same in every thread, and are kept once.
+// ------------------------------------------------------------------------------------------------
+// v of the lane that CTRL names, `none` where there is none (and in rows that ROWS leaves out): moves on the lane network, not through LDS.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u32 lane_from(u32 v, u32 none) { return (u32)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T lane_value(T v, T none) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, lane_from<CTRL, ROWS>(__builtin_bit_cast(u32, v), __builtin_bit_cast(u32, none)));
+    } else {
+        const u64 a = __builtin_bit_cast(u64, v), b = __builtin_bit_cast(u64, none);
+        return __builtin_bit_cast(T, ((u64)lane_from<CTRL, ROWS>((u32)(a >> 32), (u32)(b >> 32)) << 32) | lane_from<CTRL, ROWS>((u32)a, (u32)b));
     }
+}
+template <class T>
+__device__ __forceinline__ T last_lane(T v) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, (u32)__builtin_amdgcn_readlane((int)__builtin_bit_cast(u32, v), 63));
+    } else {
+        const u64 a = __builtin_bit_cast(u64, v);
+        return __builtin_bit_cast(T, ((u64)(u32)__builtin_amdgcn_readlane((int)(u32)(a >> 32), 63) << 32) | (u32)__builtin_amdgcn_readlane((int)(u32)a, 63));
+    }
+}
+// op over the wave's lanes in a fixed order; `none` changes nothing.
+template <class T, class Op>
+__device__ __forceinline__ T over_wave(T v, T none, Op&& op) {
+    v = op(v, lane_value<0x111, 0xf>(v, none));
+    v = op(v, lane_value<0x112, 0xf>(v, none));
+    v = op(v, lane_value<0x114, 0xf>(v, none));
+    v = op(v, lane_value<0x118, 0xf>(v, none));
+    v = op(v, lane_value<0x142, 0xa>(v, none));
+    v = op(v, lane_value<0x143, 0xc>(v, none));
+    return last_lane(v);
+}
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) { return over_wave(v, (T)0, [](T a, T b) { return a + b; }); }
+template <class T>
+__device__ __forceinline__ T wave_largest(T v) { return over_wave(v, (T)0, [](T a, T b) { return a > b ? a : b; }); }  // (whole numbers)
+template <class T>
+__device__ __forceinline__ T wave_smallest(T v) { return over_wave(v, (T)~(T)0, [](T a, T b) { return a < b ? a : b; }); }
+
+template <bool W>
+__device__ __forceinline__ SoftSum soft_wave(SoftSum a, float c) {
+    const float m = over_wave(a.m, -__builtin_inff(), [](float x, float y) { return __builtin_elementwise_maximum(x, y); });
+    soft_rescale<W>(a, m, finite_or_zero(m), c);
+    a.s = wave_sum(a.s);
+    if (W) a.w = wave_sum(a.w);
     return a;
 }
-// Over the workgroup, the same in every thread.  `sm` has an entry per wave; it may be used again after the next barrier.  (Waves' sums are joined across lanes: read by every lane,
-// those of 16 waves would take 64 registers.  Lanes of a pair may round differently, with a product and a sum fused on one side: all take the first lane's.)
-__device__ __forceinline__ SoftSum uniform(const SoftSum& a) {
-    SoftSum b;
-    b.m = uniform(a.m);
-    b.s = uniform(a.s);
-    b.w = uniform(a.w);
-    return b;
-}
-__device__ __forceinline__ double uniform(double x) {
-    const u64 v = __builtin_bit_cast(u64, x);
-    return __builtin_bit_cast(double, ((u64)(u32)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (u32)__builtin_amdgcn_readfirstlane((int)(u32)v));
-}
+// `sm` has an entry per wave; it may be used again after the next barrier.
 template <int B, bool W>
 __device__ __forceinline__ SoftSum soft_block(SoftSum a, float c, float4* sm) {
     a = soft_wave<W>(a, c);
-    if constexpr (B == 64) return uniform(a);
+    if constexpr (B == 64) return a;
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = packed(a);
     __syncthreads();
-    return uniform(soft_wave<W, B / 64>(unpacked(sm[threadIdx.x % (B / 64)]), c));
+    SoftSum b;
+    if (lane_id() < B / 64) b = unpacked(sm[lane_id()]);
+    return soft_wave<W>(b, c);
 }
 template <int B, class T>
 __device__ __forceinline__ T sum_block(T v, T* sm) {  // likewise
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    if constexpr (B == 64) return uniform(v);
+    v = wave_sum(v);
+    if constexpr (B == 64) return v;
     if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = sm[threadIdx.x % (B / 64)];
-#pragma unroll
-    for (int d = 1; d < B / 64; d *= 2) v += __shfl_xor(v, d);
-    return uniform(v);
+    return wave_sum(lane_id() < B / 64 ? sm[lane_id()] : (T)0);
 }
 
 // ------------------------------------------------------------------------------------------------
