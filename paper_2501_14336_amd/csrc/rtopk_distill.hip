@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams
     loss_of_row<DT, TAIL, kDistillFinish>(P, row, r, a, listed, sm[2], sums);
 }
 
-constexpr int kDistillGradBlock = 256, kDistillGradVecs = 4;
+constexpr int kDistillGradBlock = 256, kDistillGradVecs = 2;
 
 template <int DT>
 __global__ void __launch_bounds__(kDistillGradBlock) k_distill_grad(DistillParams P) {
@@ -171,7 +171,6 @@ constexpr int64_t kDistillMostVecs = (int64_t)1 << 15;  // (the bitmaps: a byte 
 
 // One workgroup per row, which then has its loss too, or several, and a launch more.
 constexpr int kPartBlock = 256;
-constexpr int64_t kFewRows = 512;
 static bool whole_rows(int64_t batch, int64_t n, int eb) { return (n + 14) * eb <= 16 * kDistillMostVecs && (batch >= 128 || n * eb <= 65536); }
 static RowParts distill_parts(int64_t batch, int64_t n, int eb) {
     return deal_row(batch, n, eb, kPartBlock * kDistillVecs, 2048, kDistillMostVecs);
@@ -257,7 +256,11 @@ rtopk_status rtopk_distill(const void* student, int64_t batch, int64_t n, int64_
                     hipLaunchKernelGGL((k_distill_part<DT, TAIL, B, true>), dim3(now), dim3(B), TAIL ? P.part_vecs + 3 : 0, st, P);
                 }
             };
-            auto by_block = [&](auto is_tail) { batch <= kFewRows ? of(is_tail, std::integral_constant<int, 1024>{}) : of(is_tail, std::integral_constant<int, 256>{}); };
+            auto by_block = [&](auto is_tail) {
+                if (batch <= 256) of(is_tail, std::integral_constant<int, 1024>{});
+                else if (batch <= 512) of(is_tail, std::integral_constant<int, 512>{});
+                else of(is_tail, std::integral_constant<int, 256>{});
+            };
             teacher_lse ? by_block(std::true_type{}) : by_block(std::false_type{});
             return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
         }

@@ -350,12 +350,14 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
 #pragma unroll
         for (int j = 0; j < kEach; ++j) best = max(best, e[j]);
         // the k-th best of the threads' best ones: k threads have any that are not below it, and at most kMostEntries / 256 each, which the list has room for
+        // (entries are all different, but for the zeros of threads that have none)
         top.list[threadIdx.x] = best;
+        if (threadIdx.x == 0) top.bound64[0] = 0;
         __syncthreads();
         u32 rank = 0;
 #pragma unroll 16
-        for (u32 j = 0; j < kFinishBlock; ++j) rank += top.list[j] > best || (top.list[j] == best && j < threadIdx.x);
-        if (rank == (u32)P.k - 1) top.bound64[0] = best;
+        for (u32 j = 0; j < kFinishBlock; ++j) rank += top.list[j] > best;
+        if (rank == (u32)P.k - 1 && best != 0) top.bound64[0] = best;
         __syncthreads();
         const u64 bound = top.bound64[0];
 #pragma unroll
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
 }
 
 // dx_j = (1/T) [ sum_i g_i (1[t_i = j] - p_j) - gH p_j (ln p_j + H) ]
-constexpr int kGradBlock = 256, kGradVecs = 4;
+constexpr int kGradBlock = 256, kGradVecs = 2;
 
 template <int DT, bool W>
 __global__ void __launch_bounds__(kGradBlock) k_logprobs_grad(LogprobsParams P) {
@@ -444,7 +446,7 @@ static rtopk_status make_plan(int64_t batch, int64_t n, int64_t m, int64_t k, rt
     *L = LogprobsPlan{};
     L->top = k > 0 && k <= kMostTop;
     if ((batch >= 128 && vecs <= (int64_t)kNotedVecs * 1024) || vecs <= 4096) {
-        L->block = batch > 768 && vecs <= (int64_t)kNotedVecs * 256 ? 256 : batch > 384 && vecs <= (int64_t)kNotedVecs * 512 ? 512 : 1024;
+        L->block = batch > 512 && vecs <= (int64_t)kNotedVecs * 256 ? 256 : batch > 256 && vecs <= (int64_t)kNotedVecs * 512 ? 512 : 1024;
         L->parts = 1;
         L->part_vecs = (u32)vecs;
     } else {
