@@ -15,6 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 _SRC_DIR = os.path.join(_HERE, "csrc")
 _LIB_PATH = os.path.join(_HERE, "librtopk.so")
+_TORCH_LIB_PATH = os.path.join(_HERE, "_rtopk_torch.so")
 
 RTOPK_F32, RTOPK_F16, RTOPK_BF16 = 0, 1, 2
 RTOPK_OK = 0
@@ -140,6 +141,37 @@ def build(force: bool = True) -> str:
     subprocess.check_call(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs)
     os.replace(tmp, _LIB_PATH)
     return _LIB_PATH
+
+
+def build_torch(force: bool = True) -> str:
+    """Compile the operators' entry points for torch tensors (host code, against the installed torch's headers), next to librtopk.so."""
+    src = os.path.join(_SRC_DIR, "rtopk_torch.cpp")
+    deps = [src, os.path.join(_ROOT, "include", "rtopk.h")]
+    if not force and os.path.exists(_TORCH_LIB_PATH) and all(os.path.getmtime(_TORCH_LIB_PATH) >= os.path.getmtime(d) for d in deps):
+        return _TORCH_LIB_PATH
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    tmp = _TORCH_LIB_PATH + ".tmp%d" % os.getpid()
+    subprocess.check_call(
+        ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+         "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-I", os.path.join(_ROOT, "include"), "-I", os.path.join(root, "include"),
+         "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-I", os.path.join(rocm, "include"),
+         "-I", sysconfig.get_paths()["include"], src, "-o", tmp, "-L", _HERE, "-l:librtopk.so", "-L", os.path.join(root, "lib"),
+         "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, _TORCH_LIB_PATH)
+    return _TORCH_LIB_PATH
+
+
+def load_torch():
+    """The module of the operators' entry points for torch tensors (built beforehand; built now only if it is missing)."""
+    import importlib
+    load()
+    if not os.path.exists(_TORCH_LIB_PATH):
+        build_torch(force=True)
+    return importlib.import_module(__name__.rsplit(".", 1)[0] + "._rtopk_torch")
 
 
 _lib = None

@@ -1,0 +1,330 @@
+// The operators on torch tensors: arguments are checked, outputs allocated and the C entry points of include/rtopk.h called on the current stream, without going back to Python in
+// between.  (From Python through ctypes a call with five outputs takes 18 us on the host, of which 7 are two launches; so it takes 10.)  operators.py holds what users call.
+#include <Python.h>
+
+#include <ATen/core/Tensor.h>
+#include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <cmath>
+#include <string>
+
+#include "rtopk.h"
+
+namespace {
+
+PyObject* error_type = nullptr;   // binding.RtopkError
+PyObject* memory_error = nullptr;  // torch.OutOfMemoryError
+
+struct Refused {
+    int status;
+    std::string what;
+};
+[[noreturn]] void refuse(const std::string& what) { throw Refused{RTOPK_ERR_INVALID_ARG, what}; }
+void check(rtopk_status s) {
+    if (s != RTOPK_OK) throw Refused{(int)s, rtopk_status_string(s)};
+}
+
+const at::Tensor& tensor(PyObject* o, const char* what) {
+    if (!THPVariable_Check(o)) refuse(std::string(what) + " must be a tensor");
+    return THPVariable_Unpack(o);
+}
+int64_t integer(PyObject* o, const char* what) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse(std::string(what) + " must be a whole number");
+    }
+    return v;
+}
+double number(PyObject* o, const char* what) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        refuse(std::string(what) + " must be a number");
+    }
+    return v;
+}
+float inverse(PyObject* temperature) {
+    const double t = number(temperature, "temperature");
+    if (!(t > 0.0)) refuse("temperature must be positive");
+    return (float)(1.0 / t);
+}
+rtopk_dtype type_of(const at::Tensor& x, const char* what) {
+    switch (x.scalar_type()) {
+        case at::kFloat: return RTOPK_F32;
+        case at::kHalf: return RTOPK_F16;
+        case at::kBFloat16: return RTOPK_BF16;
+        default: refuse(std::string(what) + " must be float32, float16 or bfloat16");
+    }
+}
+
+struct Rows {
+    void* p;
+    int64_t batch, n, stride;
+    rtopk_dtype dt;
+};
+Rows rows(const at::Tensor& x, const char* what) {
+    if (!x.is_cuda()) refuse(std::string(what) + " must live on the GPU; there is no CPU path");
+    if (x.dim() != 2) refuse(std::string(what) + " must be a [batch, n] tensor");
+    const int64_t batch = x.size(0), n = x.size(1);
+    if (batch < 1 || n < 1) refuse(std::string(what) + " is empty");
+    int64_t stride = n;
+    if (!x.is_contiguous()) {
+        if (batch > 1) stride = x.stride(0);
+        if ((n > 1 && x.stride(1) != 1) || stride < n) refuse(std::string(what) + " must have contiguous rows that do not overlap");
+    }
+    return Rows{x.data_ptr(), batch, n, stride, type_of(x, what)};
+}
+
+// A contiguous tensor of a shape beside the logits x; null for None.
+void* side(PyObject* o, const at::Tensor& x, int64_t size0, int64_t size1, at::ScalarType type, const char* what) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, what);
+    const bool shaped = size1 < 0 ? t.dim() == 1 && t.size(0) == size0
+                                  : (t.dim() == 2 && t.size(0) == size0 && t.size(1) == size1) || (size1 == 1 && t.dim() == 1 && t.size(0) == size0);
+    if (t.scalar_type() != type || !shaped || t.device() != x.device() || !t.is_contiguous())
+        refuse(std::string(what) + " must be a contiguous " + c10::toString(type) + " tensor of shape (" + std::to_string(size0) + (size1 < 0 ? "" : ", " + std::to_string(size1)) + ") on " +
+               x.device().str());
+    return t.data_ptr();
+}
+void* needed(PyObject* o, const at::Tensor& x, int64_t size0, int64_t size1, at::ScalarType type, const char* what) {
+    if (o == Py_None) refuse(std::string(what) + " is missing");
+    return side(o, x, size0, size1, type, what);
+}
+
+at::Tensor fresh(const at::Tensor& x, at::IntArrayRef size, at::ScalarType type = at::kFloat) { return at::detail::empty_cuda(size, type, x.device(), std::nullopt); }
+at::Tensor workspace(PyObject* given, size_t need, const at::Tensor& x) {
+    if (given != Py_None) {
+        const at::Tensor& t = tensor(given, "workspace");
+        if (t.is_contiguous() && t.device() == x.device() && t.nbytes() >= need) return t;
+    }
+    return fresh(x, {(int64_t)need}, at::kByte);
+}
+at::Tensor gradient(PyObject* given, const at::Tensor& x) {
+    if (given == Py_None) return fresh(x, x.sizes(), x.scalar_type());
+    const at::Tensor& t = tensor(given, "out");
+    if (!t.sizes().equals(x.sizes()) || t.scalar_type() != x.scalar_type() || t.device() != x.device()) refuse("out must be like the logits");
+    return t;
+}
+void* stream(const at::Tensor& x) { return (void*)c10::hip::getCurrentHIPStream(x.get_device()).stream(); }
+
+PyObject* wrapped(const at::Tensor& t) {
+    if (t.defined()) return THPVariable_Wrap(t);
+    Py_RETURN_NONE;
+}
+template <class... T>
+PyObject* tuple_of(const T&... t) {
+    PyObject* r = PyTuple_New(sizeof...(t));
+    if (!r) return nullptr;
+    Py_ssize_t i = 0;
+    bool ok = true;
+    auto put = [&](const at::Tensor& x) {
+        PyObject* o = wrapped(x);
+        ok = ok && o;
+        PyTuple_SET_ITEM(r, i++, o);
+    };
+    (put(t), ...);
+    if (ok) return r;
+    Py_DECREF(r);
+    return nullptr;
+}
+
+// f(arguments) with what it throws turned into Python's exceptions.
+template <PyObject* (*F)(PyObject* const*), int N>
+PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        if (n != N) refuse("wrong number of arguments");
+        return F(a);
+    } catch (const Refused& e) {
+        PyObject* args = Py_BuildValue("(is)", e.status, e.what.c_str());
+        if (args) {
+            PyObject* value = PyObject_CallObject(error_type, args);
+            Py_DECREF(args);
+            if (value) {
+                PyErr_SetObject(error_type, value);
+                Py_DECREF(value);
+            }
+        }
+    } catch (const c10::OutOfMemoryError& e) {
+        PyErr_SetString(memory_error, e.what_without_backtrace());
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    }
+    return nullptr;
+}
+
+// logits, tokens, k, temperature, entropy, workspace -> logprobs, top_logprobs, top_indices, entropy, row_stats
+PyObject* logprobs(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "logits");
+    const Rows r = rows(x, "logits");
+    int64_t m = 0;
+    if (a[1] != Py_None) {
+        const at::Tensor& t = tensor(a[1], "tokens");
+        m = t.dim() == 2 ? t.size(1) : 1;
+    }
+    const void* tokens = side(a[1], x, r.batch, m, at::kLong, "tokens");
+    const int64_t k = integer(a[2], "k");
+    if (k < 0 || k > r.n) refuse("k must lie between 0 and the row's length");
+    const float inv_t = inverse(a[3]);
+    const bool entropy = PyObject_IsTrue(a[4]) == 1;
+    const c10::DeviceGuard guard(x.device());
+    size_t need = 0;
+    check(rtopk_logprobs_workspace_bytes(r.batch, r.n, m, k, r.dt, &need));
+    const at::Tensor ws = workspace(a[5], need, x), lp = fresh(x, {r.batch, m}), stats = fresh(x, {r.batch, 2});
+    at::Tensor h, top, at_;
+    if (entropy) h = fresh(x, {r.batch});
+    if (k > 0) {
+        top = fresh(x, {r.batch, k});
+        at_ = fresh(x, {r.batch, k}, at::kLong);
+    }
+    check(rtopk_logprobs(r.p, r.batch, r.n, r.stride, r.dt, inv_t, (const int64_t*)tokens, m, k, (float*)lp.data_ptr(), entropy ? (float*)h.data_ptr() : nullptr,
+                         (float*)stats.data_ptr(), k > 0 ? (float*)top.data_ptr() : nullptr, k > 0 ? (int64_t*)at_.data_ptr() : nullptr, ws.data_ptr(), ws.nbytes(), stream(x)));
+    return tuple_of(lp, top, at_, h, stats);
+}
+
+// logits, tokens, row_stats, grad_logprobs, entropy, grad_entropy, temperature, out -> gradient
+PyObject* logprobs_backward(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "logits");
+    const Rows r = rows(x, "logits");
+    int64_t m = 0;
+    if (a[1] != Py_None) {
+        const at::Tensor& t = tensor(a[1], "tokens");
+        m = t.dim() == 2 ? t.size(1) : 1;
+    }
+    const void* tokens = side(a[1], x, r.batch, m, at::kLong, "tokens");
+    const void* stats = needed(a[2], x, r.batch, 2, at::kFloat, "row_stats");
+    const void* g = m > 0 ? needed(a[3], x, r.batch, m, at::kFloat, "grad_logprobs") : nullptr;
+    if (a[5] != Py_None && a[4] == Py_None) refuse("grad_entropy needs the entropy");
+    const void* h = side(a[4], x, r.batch, -1, at::kFloat, "entropy");
+    const void* gh = side(a[5], x, r.batch, -1, at::kFloat, "grad_entropy");
+    const float inv_t = inverse(a[6]);
+    const c10::DeviceGuard guard(x.device());
+    const at::Tensor out = gradient(a[7], x);
+    const Rows o = rows(out, "out");
+    check(rtopk_logprobs_backward(r.p, r.batch, r.n, r.stride, r.dt, inv_t, (const int64_t*)tokens, m, (const float*)stats, (const float*)g, (const float*)h, (const float*)gh, o.p,
+                                  o.stride, stream(x)));
+    return wrapped(out);
+}
+
+struct Lists {
+    Rows r;
+    const void *values, *columns, *lse;
+    rtopk_dtype value_dt;
+    int64_t k;
+    float inv_t;
+};
+Lists lists(const at::Tensor& x, PyObject* values, PyObject* indices, PyObject* lse, PyObject* temperature) {
+    Lists l;
+    l.r = rows(x, "student");
+    const at::Tensor& at_ = tensor(indices, "teacher_indices");
+    if (at_.dim() != 2 || at_.size(1) < 1) refuse("teacher_indices must be a [batch, k] tensor");
+    l.k = at_.size(1);
+    const at::Tensor& v = tensor(values, "teacher_values");
+    l.value_dt = type_of(v, "teacher_values");
+    l.values = side(values, x, l.r.batch, l.k, v.scalar_type(), "teacher_values");
+    l.columns = side(indices, x, l.r.batch, l.k, at::kLong, "teacher_indices");
+    l.lse = side(lse, x, l.r.batch, -1, at::kFloat, "teacher_lse");
+    l.inv_t = inverse(temperature);
+    return l;
+}
+
+// student, values, indices, lse, temperature, workspace -> loss, row_stats
+PyObject* distill(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "student");
+    const Lists l = lists(x, a[1], a[2], a[3], a[4]);
+    const c10::DeviceGuard guard(x.device());
+    size_t need = 0;
+    check(rtopk_distill_workspace_bytes(l.r.batch, l.r.n, l.k, l.r.dt, &need));
+    const at::Tensor ws = workspace(a[5], need, x), loss = fresh(x, {l.r.batch}), stats = fresh(x, {l.r.batch, RTOPK_DISTILL_ROW_STATS});
+    check(rtopk_distill(l.r.p, l.r.batch, l.r.n, l.r.stride, l.r.dt, l.inv_t, l.values, l.value_dt, (const int64_t*)l.columns, l.k, (const float*)l.lse, (float*)loss.data_ptr(),
+                        (float*)stats.data_ptr(), ws.data_ptr(), ws.nbytes(), stream(x)));
+    return tuple_of(loss, stats);
+}
+
+// student, values, indices, row_stats, grad_loss, lse, temperature, out -> gradient
+PyObject* distill_backward(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "student");
+    const Lists l = lists(x, a[1], a[2], a[5], a[6]);
+    const void* stats = needed(a[3], x, l.r.batch, RTOPK_DISTILL_ROW_STATS, at::kFloat, "row_stats");
+    const void* g = needed(a[4], x, l.r.batch, -1, at::kFloat, "grad_loss");
+    const c10::DeviceGuard guard(x.device());
+    const at::Tensor out = gradient(a[7], x);
+    const Rows o = rows(out, "out");
+    check(rtopk_distill_backward(l.r.p, l.r.batch, l.r.n, l.r.stride, l.r.dt, l.inv_t, l.values, l.value_dt, (const int64_t*)l.columns, l.k, (const float*)l.lse, (const float*)stats,
+                                 (const float*)g, o.p, o.stride, stream(x)));
+    return wrapped(out);
+}
+
+// student, values, indices, row_weights, lse, temperature, workspace, out -> loss, gradient
+PyObject* distill_step(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "student");
+    const Lists l = lists(x, a[1], a[2], a[4], a[5]);
+    const void* w = needed(a[3], x, l.r.batch, -1, at::kFloat, "row_weights");
+    const c10::DeviceGuard guard(x.device());
+    size_t need = 0;
+    check(rtopk_distill_workspace_bytes(l.r.batch, l.r.n, l.k, l.r.dt, &need));
+    const at::Tensor ws = workspace(a[6], need, x), loss = fresh(x, {l.r.batch}), out = gradient(a[7], x);
+    const Rows o = rows(out, "out");
+    check(rtopk_distill_step(l.r.p, l.r.batch, l.r.n, l.r.stride, l.r.dt, l.inv_t, l.values, l.value_dt, (const int64_t*)l.columns, l.k, (const float*)l.lse, (const float*)w,
+                             (float*)loss.data_ptr(), o.p, o.stride, ws.data_ptr(), ws.nbytes(), stream(x)));
+    return tuple_of(loss, out);
+}
+
+// logits, k, flags, bias, groups, topk_groups, scale, counts -> weights, experts
+PyObject* route(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "logits");
+    const Rows r = rows(x, "logits");
+    const int64_t k = integer(a[1], "k"), flags = integer(a[2], "flags"), groups = integer(a[4], "groups"), topk_groups = integer(a[5], "topk_groups");
+    if (k < 1 || k > r.n) refuse("k must lie between 1 and the number of experts");
+    const void* bias = side(a[3], x, r.n, -1, at::kFloat, "bias");
+    const float scale = (float)number(a[6], "scale");
+    void* counts = side(a[7], x, r.n, -1, at::kLong, "counts");
+    const c10::DeviceGuard guard(x.device());
+    const at::Tensor weights = fresh(x, {r.batch, k}), experts = fresh(x, {r.batch, k}, at::kLong);
+    check(rtopk_route(r.p, r.batch, r.n, r.stride, r.dt, (const float*)bias, groups, topk_groups, k, (uint32_t)flags, scale, (float*)weights.data_ptr(),
+                      (int64_t*)experts.data_ptr(), (int64_t*)counts, stream(x)));
+    return tuple_of(weights, experts);
+}
+
+// logits, experts, grad_weights, flags, scale, out -> gradient
+PyObject* route_backward(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "logits");
+    const Rows r = rows(x, "logits");
+    const at::Tensor& e = tensor(a[1], "experts");
+    if (e.dim() != 2) refuse("experts must be a [tokens, k] tensor");
+    const int64_t k = e.size(1);
+    const void* chosen = side(a[1], x, r.batch, k, at::kLong, "experts");
+    const void* g = needed(a[2], x, r.batch, k, at::kFloat, "grad_weights");
+    const int64_t flags = integer(a[3], "flags");
+    const float scale = (float)number(a[4], "scale");
+    const c10::DeviceGuard guard(x.device());
+    const at::Tensor out = gradient(a[5], x);
+    const Rows o = rows(out, "out");
+    check(rtopk_route_backward(r.p, r.batch, r.n, r.stride, r.dt, (const int64_t*)chosen, k, (uint32_t)flags, scale, (const float*)g, o.p, o.stride, stream(x)));
+    return wrapped(out);
+}
+
+#define ENTRY(name, count) {#name, (PyCFunction)(void (*)(void))entry<name, count>, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {
+    ENTRY(logprobs, 6), ENTRY(logprobs_backward, 8), ENTRY(distill, 6), ENTRY(distill_backward, 8), ENTRY(distill_step, 8), ENTRY(route, 8), ENTRY(route_backward, 6),
+    {nullptr, nullptr, 0, nullptr},
+};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rtopk_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+extern "C" __attribute__((visibility("default"))) PyObject* PyInit__rtopk_torch() {
+    auto from = [](const char* name, const char* attribute) -> PyObject* {
+        PyObject* m = PyImport_ImportModule(name);
+        if (!m) return nullptr;
+        PyObject* r = PyObject_GetAttrString(m, attribute);
+        Py_DECREF(m);
+        return r;
+    };
+    error_type = from("paper_2501_14336_amd.binding", "RtopkError");
+    memory_error = from("torch", "OutOfMemoryError");
+    return error_type && memory_error ? PyModule_Create(&module) : nullptr;
+}
