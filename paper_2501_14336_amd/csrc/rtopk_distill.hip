@@ -61,7 +61,7 @@ __device__ __forceinline__ void loss_of_row(const DistillParams& P, long long ro
 constexpr int kDistillVecs = 4;
 
 // Statistics of a row, or of a part of one; TAIL: apart for columns that are listed and for the others.  WHOLE: of the row, and its loss.
-template <int DT, bool TAIL, int B, bool WHOLE>
+template <int DT, bool NT, bool TAIL, int B, bool WHOLE>
 __global__ void __launch_bounds__(B) k_distill_part(DistillParams P) {
     extern __shared__ u32 marks[];  // TAIL: a byte per vector of the part, a bit per column
     __shared__ float4 sm[3][B / 64];
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(B) k_distill_part(DistillParams P) {
         }
         __syncthreads();
     }
-    sweep_vectors<DT, B, V, false>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
+    sweep_vectors<DT, B, V, NT>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
         float x[V * E];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams
 
 constexpr int kDistillGradBlock = 256, kDistillGradVecs = 2;
 
-template <int DT>
+template <int DT, bool NT>
 __global__ void __launch_bounds__(kDistillGradBlock) k_distill_grad(DistillParams P) {
     extern __shared__ __align__(16) u32 lds[];
     __shared__ u32 twice;
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kDistillGradBlock) k_distill_grad(DistillParam
         return;
     }
     const ScaledExp<DT> dense(a, d.mu, P.c);
-    write_gradient<DT, kDistillGradBlock, kDistillGradVecs, 4, false>(
+    write_gradient<DT, kDistillGradBlock, kDistillGradVecs, 4, NT>(
         r, out, aligned, v0, v1, P.k, lds, &twice, [&](long long i) { return columns[i]; },
         [&](long long i) {
             const float z = load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i));
@@ -253,7 +253,9 @@ rtopk_status rtopk_distill(const void* student, int64_t batch, int64_t n, int64_
                 constexpr int B = decltype(block)::value;
                 for (P.row0 = 0; P.row0 < batch; P.row0 += kMostWorkgroups) {
                     const unsigned now = (unsigned)(batch - P.row0 < kMostWorkgroups ? batch - P.row0 : kMostWorkgroups);
-                    hipLaunchKernelGGL((k_distill_part<DT, TAIL, B, true>), dim3(now), dim3(B), TAIL ? P.part_vecs + 3 : 0, st, P);
+                    const size_t lds = TAIL ? P.part_vecs + 3 : 0;
+                    if (past_caches(batch, n, RowElem<DT>::kBytes)) hipLaunchKernelGGL((k_distill_part<DT, true, TAIL, B, true>), dim3(now), dim3(B), lds, st, P);
+                    else hipLaunchKernelGGL((k_distill_part<DT, false, TAIL, B, true>), dim3(now), dim3(B), lds, st, P);
                 }
             };
             auto by_block = [&](auto is_tail) {
@@ -269,7 +271,7 @@ rtopk_status rtopk_distill(const void* student, int64_t batch, int64_t n, int64_
             const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
             auto of = [&](auto is_tail) {
                 constexpr bool TAIL = decltype(is_tail)::value;
-                hipLaunchKernelGGL((k_distill_part<DT, TAIL, kPartBlock, false>), dim3(now * d.parts), dim3(kPartBlock), TAIL ? d.vecs : 0, st, P);
+                hipLaunchKernelGGL((k_distill_part<DT, false, TAIL, kPartBlock, false>), dim3(now * d.parts), dim3(kPartBlock), TAIL ? d.vecs : 0, st, P);
                 hipLaunchKernelGGL((k_distill_finish<DT, TAIL>), dim3(now), dim3(kDistillFinish), 0, st, P);
             };
             teacher_lse ? of(std::true_type{}) : of(std::false_type{});
@@ -303,7 +305,8 @@ rtopk_status rtopk_distill_backward(const void* student, int64_t batch, int64_t 
         const size_t lds = gradient_lds<DT, kDistillGradBlock, kDistillGradVecs>(d.vecs);
         for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
             const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
-            hipLaunchKernelGGL((k_distill_grad<DT>), dim3(now * d.parts), dim3(kDistillGradBlock), lds, (hipStream_t)hip_stream, P);
+            if (past_caches(batch, n, eb)) hipLaunchKernelGGL((k_distill_grad<DT, true>), dim3(now * d.parts), dim3(kDistillGradBlock), lds, (hipStream_t)hip_stream, P);
+            else hipLaunchKernelGGL((k_distill_grad<DT, false>), dim3(now * d.parts), dim3(kDistillGradBlock), lds, (hipStream_t)hip_stream, P);
         }
         return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
     });

@@ -186,7 +186,7 @@ __device__ __forceinline__ void write_top(const LogprobsParams& P, long long row
 
 struct NoTop {};
 
-template <int DT, int B, int V, bool W, bool TOP, bool WHOLE>
+template <int DT, int B, int V, bool NT, bool W, bool TOP, bool WHOLE>
 __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
     constexpr int E = RowElem<DT>::E;
     __shared__ float4 sm[B / 64];
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
             }
         }
     };
-    sweep_vectors<DT, B, V, false>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
+    sweep_vectors<DT, B, V, NT>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
         float x[V * E], most[V], t = a.m;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -335,6 +335,7 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
     const u32 entries = TOP ? P.parts * (u32)P.k : 0u;
     constexpr int kEach = TOP ? kMostEntries / kFinishBlock : 1;
     u64 e[kEach], best = 0;
+    const u64 head = TOP && threadIdx.x < P.parts ? lists[threadIdx.x * (u32)P.k] : 0;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         const u32 i = j * kFinishBlock + threadIdx.x;
@@ -349,15 +350,19 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
         if (threadIdx.x == 0) top.count = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) best = max(best, e[j]);
-        // the k-th best of the threads' best ones: k threads have any that are not below it, and at most kMostEntries / 256 each, which the list has room for
-        // (entries are all different, but for the zeros of threads that have none)
-        top.list[threadIdx.x] = best;
+        // A bound: where there are parts enough and k is small, the k-th best of the parts' first entries (k parts have any that are not below it, at most k each); else the k-th best
+        // of the threads' best ones (k threads have any, at most kMostEntries / 256 each).  The list has room for either.  (Entries are all different, but for the zeros of parts and
+        // threads that have none.)
+        const bool by_heads = P.parts >= (u32)P.k && P.parts <= kFinishBlock && (u32)(P.k * P.k) <= kListRoom;
+        const u64 mine = by_heads ? head : best;
+        const u32 others = by_heads ? P.parts : kFinishBlock;
+        top.list[threadIdx.x] = mine;
         if (threadIdx.x == 0) top.bound64[0] = 0;
         __syncthreads();
         u32 rank = 0;
 #pragma unroll 16
-        for (u32 j = 0; j < kFinishBlock; ++j) rank += top.list[j] > best;
-        if (rank == (u32)P.k - 1 && best != 0) top.bound64[0] = best;
+        for (u32 j = 0; j < others; ++j) rank += top.list[j] > mine;
+        if (rank == (u32)P.k - 1 && mine != 0 && threadIdx.x < others) top.bound64[0] = mine;
         __syncthreads();
         const u64 bound = top.bound64[0];
 #pragma unroll
@@ -385,7 +390,7 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
 // dx_j = (1/T) [ sum_i g_i (1[t_i = j] - p_j) - gH p_j (ln p_j + H) ]
 constexpr int kGradBlock = 256, kGradVecs = 2;
 
-template <int DT, bool W>
+template <int DT, bool NT, bool W>
 __global__ void __launch_bounds__(kGradBlock) k_logprobs_grad(LogprobsParams P) {
     extern __shared__ __align__(16) u32 lds[];
     __shared__ u32 twice;
@@ -406,7 +411,7 @@ __global__ void __launch_bounds__(kGradBlock) k_logprobs_grad(LogprobsParams P) 
     const float inv_s = s == 0.0f ? 0.0f : 1.0f / s, log2_s = s == 0.0f ? 0.0f : log2_fast(s);
     const float a = -sum * P.inv_t * inv_s, b = -gh * P.inv_t * kLn2 * inv_s, h2 = W ? P.entropy[row] * (1.0f / kLn2) - log2_s : 0.0f;
     const ScaledExp<DT> dense(a, ref, P.c);
-    write_gradient<DT, kGradBlock, kGradVecs, 1, false>(
+    write_gradient<DT, kGradBlock, kGradVecs, 1, NT>(
         r, out, (((uintptr_t)out ^ (uintptr_t)r.x) & 15) == 0, v0, v1, P.m, lds, &twice, [&](long long i) { return tokens[i]; },
         [&](long long i) { return g[i]; },
         [&](float (&x)[RowElem<DT>::E]) {
@@ -432,6 +437,7 @@ constexpr int64_t kLogprobsMostVecs = (int64_t)1 << 15;  // (the gradient's bitm
 struct LogprobsPlan {
     bool top;    // alternatives by the sweep itself (otherwise rtopk_select finds them first)
     int block;   // a workgroup of so many threads takes a row; 0: several share one, and a second launch puts their parts together
+    bool past_caches;  // rows are read past the caches
     u32 parts, part_vecs;
     size_t partial_bytes, top_bytes, select_bytes;
     size_t bytes() const { return partial_bytes + top_bytes + select_bytes; }
@@ -447,6 +453,7 @@ static rtopk_status make_plan(int64_t batch, int64_t n, int64_t m, int64_t k, rt
     L->top = k > 0 && k <= kMostTop;
     if ((batch >= 128 && vecs <= (int64_t)kNotedVecs * 1024) || vecs <= 4096) {
         L->block = batch > 512 && vecs <= (int64_t)kNotedVecs * 256 ? 256 : batch > 256 && vecs <= (int64_t)kNotedVecs * 512 ? 512 : 1024;
+        L->past_caches = past_caches(batch, n, eb);
         L->parts = 1;
         L->part_vecs = (u32)vecs;
     } else {
@@ -480,11 +487,16 @@ static void launch_logprobs(LogprobsParams P, const LogprobsPlan& L, int64_t bat
     const int64_t rows = kMostWorkgroups / L.parts > 0 ? kMostWorkgroups / L.parts : 1;
     for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
         const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
-        if (L.block == 256) hipLaunchKernelGGL((k_logprobs_sweep<DT, 256, kWholeVecs, W, TOP, true>), dim3(now), dim3(256), 0, st, P);
-        else if (L.block == 512) hipLaunchKernelGGL((k_logprobs_sweep<DT, 512, kWholeVecs, W, TOP, true>), dim3(now), dim3(512), 0, st, P);
-        else if (L.block == 1024) hipLaunchKernelGGL((k_logprobs_sweep<DT, 1024, kWholeVecs, W, TOP, true>), dim3(now), dim3(1024), 0, st, P);
+        auto whole = [&](auto block) {
+            constexpr int B = decltype(block)::value;
+            if (L.past_caches) hipLaunchKernelGGL((k_logprobs_sweep<DT, B, kWholeVecs, true, W, TOP, true>), dim3(now), dim3(B), 0, st, P);
+            else hipLaunchKernelGGL((k_logprobs_sweep<DT, B, kWholeVecs, false, W, TOP, true>), dim3(now), dim3(B), 0, st, P);
+        };
+        if (L.block == 256) whole(std::integral_constant<int, 256>{});
+        else if (L.block == 512) whole(std::integral_constant<int, 512>{});
+        else if (L.block == 1024) whole(std::integral_constant<int, 1024>{});
         else {
-            hipLaunchKernelGGL((k_logprobs_sweep<DT, kPartBlock, kPartVecs, W, TOP, false>), dim3(now * L.parts), dim3(kPartBlock), 0, st, P);
+            hipLaunchKernelGGL((k_logprobs_sweep<DT, kPartBlock, kPartVecs, false, W, TOP, false>), dim3(now * L.parts), dim3(kPartBlock), 0, st, P);
             hipLaunchKernelGGL((k_logprobs_finish<DT, W, TOP>), dim3(now), dim3(kFinishBlock), 0, st, P);
         }
     }
@@ -595,8 +607,11 @@ rtopk_status rtopk_logprobs_backward(const void* logits, int64_t batch, int64_t 
         const size_t lds = m > 0 ? gradient_lds<DT, kGradBlock, kGradVecs>(d.vecs) : 0;
         for (P.row0 = 0; P.row0 < batch; P.row0 += rows) {
             const unsigned now = (unsigned)(batch - P.row0 < rows ? batch - P.row0 : rows);
-            if (grad_entropy) hipLaunchKernelGGL((k_logprobs_grad<DT, true>), dim3(now * d.parts), dim3(kGradBlock), lds, (hipStream_t)hip_stream, P);
-            else hipLaunchKernelGGL((k_logprobs_grad<DT, false>), dim3(now * d.parts), dim3(kGradBlock), lds, (hipStream_t)hip_stream, P);
+            auto go = [&](auto nt, auto w) {
+                hipLaunchKernelGGL((k_logprobs_grad<DT, decltype(nt)::value, decltype(w)::value>), dim3(now * d.parts), dim3(kGradBlock), lds, (hipStream_t)hip_stream, P);
+            };
+            if (past_caches(batch, n, eb)) grad_entropy ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+            else grad_entropy ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
         }
         return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
     });
