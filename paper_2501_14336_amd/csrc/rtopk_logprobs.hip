@@ -48,10 +48,12 @@ __device__ __forceinline__ u32 key_of(float x) { return KeyOf<RTOPK_F32>::key(__
 __device__ __forceinline__ float number_of(u32 key) { return __uint_as_float((key & 0x80000000u) ? (key ^ 0x80000000u) : ~key); }  // (the key of all NaNs gives one)
 __device__ __forceinline__ u64 entry_of(u32 key, u32 col) { return ((u64)key << 32) | (u32)~col; }
 
-// A bound that at least `want` of the workgroup's threads' values are not below, if there are as many values; 0 if not.  `sm` has an entry per wave and is free after the next barrier.
+// A bound that at least `want` (up to 64) of the workgroup's threads' values are not below; 0 where `threads`, the first so many that have one, do not fill a wave.  `sm` has an entry
+// per wave and is free after the next barrier.
 template <int B, class T>
-__device__ __forceinline__ T bound_of_threads(T v, u32 want, T* sm) {
-    const u32 of_wave = (want + B / 64 - 1) / (B / 64);
+__device__ __forceinline__ T bound_of_threads(T v, u32 threads, u32 want, T* sm) {
+    const u32 waves = min(threads, (u32)B) / 64;  // full ones: the rest may hold anything
+    const u32 of_wave = waves == 0 ? 0 : (want + waves - 1) / waves;
     T best = 0;
     for (u32 i = 0; i < of_wave; ++i) {
         best = wave_largest(v);
@@ -60,7 +62,7 @@ __device__ __forceinline__ T bound_of_threads(T v, u32 want, T* sm) {
     }
     if (lane_id() == 0) sm[threadIdx.x >> 6] = best;
     __syncthreads();
-    return wave_smallest(sm[lane_id() % (B / 64)]);
+    return waves == 0 ? (T)0 : wave_smallest(sm[lane_id() % (B / 64) < waves ? lane_id() % (B / 64) : 0]);
 }
 
 template <int B>
@@ -235,7 +237,7 @@ __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
         soft_add_to<W>(a, x, t, P.c);
         if constexpr (TOP) {
             if (first == v0) {
-                bound = bound_of_threads<B>(first + threadIdx.x < v1 ? key_of(a.m) : 0u, (u32)P.k, top.bound);
+                bound = bound_of_threads<B>(key_of(a.m), v1 - v0, (u32)P.k, top.bound);
                 bound_number = bound == 0 ? -__builtin_inff() : number_of(bound);
             }
             u32 hits = 0;
@@ -264,7 +266,7 @@ __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
         const long long here = (long long)min((u64)v1 * E, (u64)r.lead + r.n) - (long long)max((u64)v0 * E, (u64)r.lead);  // columns
         const u32 want = here < P.k ? (here < 0 ? 0u : (u32)here) : (u32)P.k;
         if (!one_tile) {
-            bound = max(bound, bound_of_threads<B>(key_of(mine), (u32)P.k, (u32*)top.bound64));
+            bound = max(bound, bound_of_threads<B>(key_of(mine), B, (u32)P.k, (u32*)top.bound64));
             bound_number = bound == 0 ? -__builtin_inff() : number_of(bound);
             if (!(mine < bound_number)) {
                 while (noted) {
@@ -452,7 +454,7 @@ static rtopk_status make_plan(int64_t batch, int64_t n, int64_t m, int64_t k, rt
     *L = LogprobsPlan{};
     L->top = k > 0 && k <= kMostTop;
     if ((batch >= 128 && vecs <= (int64_t)kNotedVecs * 1024) || vecs <= 4096) {
-        L->block = batch > 512 && vecs <= (int64_t)kNotedVecs * 256 ? 256 : batch > 256 && vecs <= (int64_t)kNotedVecs * 512 ? 512 : 1024;
+        L->block = vecs <= 256 * kWholeVecs || (batch > 512 && vecs <= (int64_t)kNotedVecs * 256) ? 256 : batch > 256 && vecs <= (int64_t)kNotedVecs * 512 ? 512 : 1024;
         L->past_caches = past_caches(batch, n, eb);
         L->parts = 1;
         L->part_vecs = (u32)vecs;

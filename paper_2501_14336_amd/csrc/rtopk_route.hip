@@ -65,27 +65,43 @@ __device__ __forceinline__ void wave_sync() {
 
 __device__ __forceinline__ float number_of_f32_key(u32 o) { return __uint_as_float((o & 0x80000000u) ? (o ^ 0x80000000u) : ~o); }
 
-// A lane's logits, -inf beyond the row.  `aligned`: rows start on a multiple of the lane's bytes, 16 at most.
-template <int DT, int N>
-__device__ __forceinline__ void lane_logits(const char* row, u32 first, u32 experts, bool aligned, float (&x)[N]) {
+// A lane's logits, -inf beyond the row.  `aligned`: rows start on a multiple of the lane's bytes, 16 at most; otherwise the token's lanes fetch neighbouring elements and change them
+// by way of `stage` (56182 tokens of 198 bf16 experts, both passes: 100 us with every lane fetching its own).
+template <int DT, int L, int N>
+__device__ __forceinline__ void lane_logits(const char* row, u32 l, u32 experts, bool aligned, float* stage, float (&x)[N]) {
     constexpr int kBytes = N * RowElem<DT>::kBytes, kWord = kBytes < 16 ? kBytes : 16;
+    const u32 first = l * N;
     if constexpr (kBytes >= 4) {
-        if (aligned && first + N <= experts) {
-            union { u32 w[kBytes / 4]; uint16_t h[kBytes / 2]; } q;
+        if (aligned) {
+            if (first + N <= experts) {
+                u32 w[kBytes / 4];
 #pragma unroll
-            for (int i = 0; i < kBytes / kWord; ++i) {
-                const char* p = row + (size_t)first * RowElem<DT>::kBytes + i * kWord;
-                if constexpr (kWord == 16) *(u32x4*)&q.w[i * 4] = *(const u32x4*)p;
-                else if constexpr (kWord == 8) *(uint2*)&q.w[0] = *(const uint2*)p;
-                else q.w[0] = *(const u32*)p;
+                for (int i = 0; i < kBytes / kWord; ++i) {
+                    const char* p = row + (size_t)first * RowElem<DT>::kBytes + i * kWord;
+                    if constexpr (kWord == 16) *(u32x4*)&w[i * 4] = *(const u32x4*)p;
+                    else if constexpr (kWord == 8) *(uint2*)&w[0] = *(const uint2*)p;
+                    else w[0] = *(const u32*)p;
+                }
+#pragma unroll
+                for (int j = 0; j < N; ++j) x[j] = RowElem<DT>::from_bits(DT == RTOPK_F32 ? w[j] : (w[j / 2] >> (j & 1 ? 16 : 0)) & 0xffffu);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) x[j] = first + j < experts ? RowElem<DT>::load(row, first + j) : -__builtin_inff();
             }
-#pragma unroll
-            for (int j = 0; j < N; ++j) x[j] = RowElem<DT>::from_bits(DT == RTOPK_F32 ? q.w[j] : (q.w[j / 2] >> (j & 1 ? 16 : 0)) & 0xffffu);
             return;
         }
     }
+    typedef RouteShape<L, N> S;
+    wave_sync();  // (what the stage held has been read)
+    float t[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = first + j < experts ? RowElem<DT>::load(row, first + j) : -__builtin_inff();
+    for (int j = 0; j < N; ++j) t[j] = j * L + l < experts ? RowElem<DT>::load(row, j * L + l) : -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < N; ++j) stage[S::place(j * L + l)] = t[j];
+    wave_sync();
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = stage[S::place(first + j)];
+    wave_sync();
 }
 
 // Scores of a lane's experts; all zero in a row without anything but -inf.
@@ -175,8 +191,8 @@ __global__ void __launch_bounds__(B) k_route(RouteParams P) {
         u32 l = lane % L;
         asm volatile("" : "+v"(l));  // (what depends on the lane alone is made anew for every token: kept, it takes more registers than there are)
         float x[N], s[N], bias[N];
-        lane_logits<DT, N>(P.logits + row * P.row_bytes, l * N, P.experts, aligned, x);
-        if (P.bias) lane_logits<RTOPK_F32, N>((const char*)P.bias, l * N, P.experts, ((uintptr_t)P.bias & (kBiasWord - 1)) == 0, bias);
+        lane_logits<DT, L, N>(P.logits + row * P.row_bytes, l, P.experts, aligned, mine, x);
+        if (P.bias) lane_logits<RTOPK_F32, L, N>((const char*)P.bias, l, P.experts, ((uintptr_t)P.bias & (kBiasWord - 1)) == 0, mine, bias);
         scores_of<L, N>(x, s, sigmoid);
         u32 key[N];  // orders the choice; 0 for what may not be chosen
 #pragma unroll
@@ -329,7 +345,7 @@ __global__ void __launch_bounds__(kRouteGradBlock) k_route_grad(RouteParams P) {
         const bool there = e >= 0 && e < (long long)P.experts;
         float g = there ? P.scale * P.grad_weights[row * P.k + l] : 0.0f;
         float x[N], s[N];
-        lane_logits<DT, N>(P.logits + row * P.row_bytes, l * N, P.experts, aligned, x);
+        lane_logits<DT, L, N>(P.logits + row * P.row_bytes, l, P.experts, aligned, mine, x);
         scores_of<L, N>(x, s, sigmoid);
         wave_sync();  // (the last tokens' sums have been read)
 #pragma unroll
@@ -352,27 +368,30 @@ __global__ void __launch_bounds__(kRouteGradBlock) k_route_grad(RouteParams P) {
         if (token < P.tokens) {
             char* out = P.grad + row * P.grad_bytes;
             constexpr int kBytes = N * RowElem<DT>::kBytes;
-            bool stored = false;
             if constexpr (kBytes >= 4) {
                 if (aligned_out && l * N + N <= P.experts) {
-                    union { u32 w[kBytes / 4]; uint16_t h[kBytes / 2]; } q;
+                    u32 w[kBytes / 4];
 #pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const u32 b = RowElem<DT>::to_bits(mine[S::place(l * N + j)]);
-                        if constexpr (DT == RTOPK_F32) q.w[j] = b;
-                        else q.w[j / 2] = j & 1 ? q.w[j / 2] | (b << 16) : b;
+                    for (int j = 0; j < N; j += DT == RTOPK_F32 ? 1 : 2) {
+                        const float a = mine[S::place(l * N + j)], b = DT == RTOPK_F32 ? 0.0f : mine[S::place(l * N + j + 1)];
+                        if constexpr (DT == RTOPK_F32) w[j] = __float_as_uint(a);
+                        else w[j / 2] = RowElem<DT>::pack2(a, b);
                     }
 #pragma unroll
                     for (int i = 0; i < kBytes / (int)kWord; ++i) {
                         char* p = out + (size_t)l * kBytes + i * kWord;
-                        if constexpr (kWord == 16) *(u32x4*)p = *(const u32x4*)&q.w[i * 4];
-                        else if constexpr (kWord == 8) *(uint2*)p = *(const uint2*)&q.w[0];
-                        else *(u32*)p = q.w[0];
+                        if constexpr (kWord == 16) *(u32x4*)p = *(const u32x4*)&w[i * 4];
+                        else if constexpr (kWord == 8) *(uint2*)p = *(const uint2*)&w[0];
+                        else *(u32*)p = w[0];
                     }
-                    stored = true;
                 }
             }
-            if (!stored) {
+            // (lanes that hold the row's last ones, and rows that are not aligned: neighbouring elements at a time)
+            if (!aligned_out || kBytes < 4) {
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (j * L + l < P.experts) RowElem<DT>::store(out, j * L + l, mine[S::place(j * L + l)]);
+            } else if (l * N + N > P.experts) {
 #pragma unroll
                 for (int j = 0; j < N; ++j)
                     if (l * N + j < P.experts) RowElem<DT>::store(out, l * N + j, mine[S::place(l * N + j)]);
@@ -444,7 +463,7 @@ rtopk_status rtopk_route(const void* logits, int64_t tokens, int64_t experts, in
                 hipLaunchKernelGGL((k_route<DT, L, N, B>), dim3((unsigned)(wgs < most ? wgs : most)), dim3(B), 0, (hipStream_t)hip_stream, P);
             };
             // Tokens are counted in LDS first.  Adds to one line of memory take 11 ns each, whoever makes them, so where they are counted few and large workgroups take all of them.
-            if (counts) launch(std::integral_constant<int, 1024>{}, 256);
+            if (counts && tokens > 4096) launch(std::integral_constant<int, 1024>{}, 256);
             else launch(std::integral_constant<int, 256>{}, 2048);
             return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
         });
