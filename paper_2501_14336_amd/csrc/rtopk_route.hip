@@ -33,9 +33,6 @@ struct RouteShape {
     static constexpr u32 place(u32 e) { return e + e / 32; }  // of an expert's word
 };
 
-// 1 / (1 + e^-x) in the steps that a 32-bit program takes, each rounded: what is chosen by it is chosen alike everywhere.
-__device__ __forceinline__ float sigmoid_of(float x) { return 1.0f / (1.0f + expf(-x)); }
-
 // Over a token's lanes, the same in all of them: rotations within rows of 16 lanes pair the same two sums in every lane.
 template <int CTRL>
 __device__ __forceinline__ u32 row_rotated(u32 v) { return (u32)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false); }
@@ -104,12 +101,37 @@ __device__ __forceinline__ void lane_logits(const char* row, u32 l, u32 experts,
     wave_sync();
 }
 
-// Scores of a lane's experts; all zero in a row without anything but -inf.
+// 1 / d and a / d as a division rounds them (Markstein's theorem: a reciprocal that is off by one unit, put right by its residual, is the rounded one, and so is a quotient put right
+// by that), in 3 instructions each where a division takes 10: for d from 1 to 2^125, and quotients whose residual is no denormal.
+__device__ __forceinline__ float rounded_reciprocal(float d) {
+    const float r = __builtin_amdgcn_rcpf(d);
+    return __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
+}
+__device__ __forceinline__ float rounded_quotient(float a, float d, float reciprocal) {
+    const float q = a * reciprocal;
+    return __builtin_fmaf(__builtin_fmaf(-q, d, a), reciprocal, q);
+}
+
+// Scores of a lane's experts, in the steps that a 32-bit program takes, each rounded: what is chosen by them is chosen alike everywhere.  All zero in a row without anything but -inf.
 template <int L, int N>
 __device__ __forceinline__ void scores_of(const float (&x)[N], float (&s)[N], bool sigmoid) {
     if (sigmoid) {
+        float d[N];
+        bool ordinary = true;
 #pragma unroll
-        for (int j = 0; j < N; ++j) s[j] = sigmoid_of(x[j]);
+        for (int j = 0; j < N; ++j) {
+            d[j] = x[j] == -__builtin_inff() ? 1.0f : 1.0f + expf(-x[j]);
+            ordinary &= d[j] <= 0x1p125f;
+        }
+        if (ordinary) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) s[j] = rounded_reciprocal(d[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) s[j] = 1.0f / d[j];
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = x[j] == -__builtin_inff() ? 0.0f : s[j];
         return;
     }
     float m = x[0];
@@ -120,8 +142,14 @@ __device__ __forceinline__ void scores_of(const float (&x)[N], float (&s)[N], bo
 #pragma unroll
     for (int j = 0; j < N; ++j) sum += s[j] = expf(x[j] - m);
     sum = token_reduce<L>(sum, AddOf{});
+    if (sum >= 1.0f && sum <= 0x1p20f) {
+        const float reciprocal = rounded_reciprocal(sum);
 #pragma unroll
-    for (int j = 0; j < N; ++j) s[j] = sum == 0.0f ? 0.0f : s[j] / sum;
+        for (int j = 0; j < N; ++j) s[j] = rounded_quotient(s[j], sum, reciprocal);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = sum == 0.0f ? 0.0f : s[j] / sum;
+    }
 }
 
 // A choice: its key above the complement of its expert, 42 bits, so that all are different and the larger is the better one.  The same bits read as a 64-bit float are one of the numbers
@@ -142,9 +170,9 @@ __device__ __forceinline__ double smaller(double a, double b) {
     return r;
 }
 
-// Best first (odd-even merge sort).
+// Best first (odd-even merge sort) of c[0 .. N).
 template <int N>
-__device__ __forceinline__ void sort_choices(double (&c)[N]) {
+__device__ __forceinline__ void sort_choices(double* c) {
 #pragma unroll
     for (int p = 1; p < N; p *= 2)
 #pragma unroll
@@ -159,20 +187,90 @@ __device__ __forceinline__ void sort_choices(double (&c)[N]) {
                         c[i + j + k] = smaller(a, b);
                     }
 }
-
 template <int CTRL>
 __device__ __forceinline__ u32 lane_swapped(u32 v) { return (u32)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false); }
+// The K best of a and b, best first as they are, in a: the larger of each pair from opposite ends, which fall and then rise, put in order.
+template <int K>
+__device__ __forceinline__ void merge_choices(double* a, const double* b) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) a[i] = larger(a[i], b[K - 1 - i]);
+#pragma unroll
+    for (int d = K / 2; d >= 1; d /= 2)
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (!(i & d)) {
+                const double x = a[i], y = a[i + d];
+                a[i] = larger(x, y);
+                a[i + d] = smaller(x, y);
+            }
+}
+// The K best of the N in c, best first, in its first places: runs of K are sorted and merged.
+template <int K, int N>
+__device__ __forceinline__ void best_of_lane(double* c) {
+    if constexpr (N == K) {
+        sort_choices<N>(c);
+    } else {
+        best_of_lane<K, N / 2>(c);
+        best_of_lane<K, N / 2>(c + N / 2);
+        merge_choices<K>(c, c + N / 2);
+    }
+}
+__device__ __forceinline__ double choice_from(u32 low, u32 high) { return __builtin_bit_cast(double, ((u64)high << 32) | low); }
+// The K best of the token's lanes, each of which has K, best first, in c: the same in all of them.  Lanes 1, 2, a half row and a row apart change theirs; rows of 16, and halves of the
+// wave, are exchanged by the instructions for it.
+template <int CTRL, int K>
+__device__ __forceinline__ void merge_lanes(double* c) {
+    double b[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const u64 v = __builtin_bit_cast(u64, c[i]);
+        b[i] = choice_from(lane_swapped<CTRL>((u32)v), lane_swapped<CTRL>((u32)(v >> 32)));
+    }
+    merge_choices<K>(c, b);
+}
+template <int ROWS, int K>
+__device__ __forceinline__ void merge_rows(double* c) {
+    double b[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const u64 v = __builtin_bit_cast(u64, c[i]);
+        auto swapped = [](u32 w) {
+            if constexpr (ROWS == 1) return __builtin_amdgcn_permlane16_swap(w, w, false, false);
+            else return __builtin_amdgcn_permlane32_swap(w, w, false, false);
+        };
+        const auto low = swapped((u32)v), high = swapped((u32)(v >> 32));
+        c[i] = choice_from(low[0], high[0]);
+        b[i] = choice_from(low[1], high[1]);
+    }
+    merge_choices<K>(c, b);
+}
+template <int L, int K>
+__device__ __forceinline__ void best_of_token(double* c) {
+    merge_lanes<0xb1, K>(c);
+    merge_lanes<0x4e, K>(c);
+    merge_lanes<0x141, K>(c);
+    merge_lanes<0x140, K>(c);
+    if constexpr (L == 64) {
+        merge_rows<1, K>(c);
+        merge_rows<2, K>(c);
+    }
+}
+
 // The two best keys of two sets.
 __device__ __forceinline__ void best_two(u32& a, u32& b, u32 a2, u32 b2) {
     b = max(min(a, a2), max(b, b2));
     a = max(a, a2);
 }
 
-template <int DT, int L, int N, int B>
-__global__ void __launch_bounds__(B) k_route(RouteParams P) {
+// Workgroups of up to kRouteBlock threads; LDS: a token's words for each of its L threads, and a word per expert where tokens are counted.
+constexpr int kRouteBlock = 1024;
+
+template <int DT, int L, int N, int K>
+__global__ void __launch_bounds__(kRouteBlock) k_route(RouteParams P) {
     typedef RouteShape<L, N> S;
-    __shared__ float stage[B / L][S::kStage];
-    __shared__ u32 tally[L * N];  // what this workgroup's tokens chose
+    HIP_DYNAMIC_SHARED(float, stage)
+    const u32 B = blockDim.x;
+    u32* const tally = (u32*)(stage + B / L * S::kStage);  // what this workgroup's tokens chose
     const u32 lane = lane_id(), slot = threadIdx.x / L;
     const bool sigmoid = (P.flags & RTOPK_ROUTE_SIGMOID) != 0, top2 = (P.flags & RTOPK_ROUTE_GROUP_TOP2) != 0;
     constexpr u32 kWord = N * RowElem<DT>::kBytes < 16 ? N * RowElem<DT>::kBytes : 16, kBiasWord = N * 4 < 16 ? N * 4 : 16;
@@ -184,7 +282,7 @@ __global__ void __launch_bounds__(B) k_route(RouteParams P) {
         for (u32 i = threadIdx.x; i < P.experts; i += B) tally[i] = 0;
         __syncthreads();
     }
-    float* const mine = stage[slot];
+    float* const mine = stage + slot * S::kStage;
     for (long long first = (long long)blockIdx.x * (B / L); first < P.tokens; first += (long long)gridDim.x * (B / L)) {
         // (lanes of a token that is none work on the last one's row, and store nothing)
         const long long token = first + slot, row = token < P.tokens ? token : P.tokens - 1;
@@ -278,32 +376,43 @@ __global__ void __launch_bounds__(B) k_route(RouteParams P) {
         wave_sync();
 #pragma unroll
         for (int j = 0; j < N; ++j) mine[S::place(l * N + j)] = s[j];
-        // every lane's choices in order; the best of the lanes' first is taken k times
-        double c[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) c[j] = choice_of(key[j], l * N + j);
-        sort_choices(c);
         u32 e = 0;
-#pragma clang loop unroll(disable)
-        for (u32 r = 0; r < P.k; ++r) {
-            double top = c[0];
-            auto across = [&](auto ctrl) {
-                const u64 v = __builtin_bit_cast(u64, top);
-                top = larger(top, __builtin_bit_cast(double, ((u64)row_rotated<decltype(ctrl)::value>((u32)(v >> 32)) << 32) | row_rotated<decltype(ctrl)::value>((u32)v)));
-            };
-            across(std::integral_constant<int, 0x128>{});
-            across(std::integral_constant<int, 0x124>{});
-            across(std::integral_constant<int, 0x122>{});
-            across(std::integral_constant<int, 0x121>{});
-            if constexpr (L == 64) {
-                top = larger(top, __shfl_xor(top, 16));
-                top = larger(top, __shfl_xor(top, 32));
-            }
-            if (l == r) e = expert_of(top);
-            if (__builtin_bit_cast(u64, c[0]) == __builtin_bit_cast(u64, top)) {
+        if constexpr (K > 0) {
+            // every lane's K best in order, merged across the token's lanes
+            double c[N];
 #pragma unroll
-                for (int j = 0; j + 1 < N; ++j) c[j] = c[j + 1];
-                c[N - 1] = 0.0;
+            for (int j = 0; j < N; ++j) c[j] = choice_of(key[j], l * N + j);
+            best_of_lane<K, N>(c);
+            best_of_token<L, K>(c);
+#pragma unroll
+            for (int r = 0; r < K; ++r) e = l == (u32)r ? expert_of(c[r]) : e;
+        } else {
+            // every lane's choices in order; the best of the lanes' first is taken k times
+            double c[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) c[j] = choice_of(key[j], l * N + j);
+            sort_choices<N>(c);
+#pragma clang loop unroll(disable)
+            for (u32 r = 0; r < P.k; ++r) {
+                double top = c[0];
+                auto across = [&](auto ctrl) {
+                    const u64 v = __builtin_bit_cast(u64, top);
+                    top = larger(top, choice_from(row_rotated<decltype(ctrl)::value>((u32)v), row_rotated<decltype(ctrl)::value>((u32)(v >> 32))));
+                };
+                across(std::integral_constant<int, 0x128>{});
+                across(std::integral_constant<int, 0x124>{});
+                across(std::integral_constant<int, 0x122>{});
+                across(std::integral_constant<int, 0x121>{});
+                if constexpr (L == 64) {
+                    top = larger(top, __shfl_xor(top, 16));
+                    top = larger(top, __shfl_xor(top, 32));
+                }
+                if (l == r) e = expert_of(top);
+                if (__builtin_bit_cast(u64, c[0]) == __builtin_bit_cast(u64, top)) {
+#pragma unroll
+                    for (int j = 0; j + 1 < N; ++j) c[j] = c[j + 1];
+                    c[N - 1] = 0.0;
+                }
             }
         }
         wave_sync();
@@ -423,6 +532,20 @@ static rtopk_status by_experts(int64_t experts, int64_t k, F&& f) {
     return f(lanes, std::integral_constant<int, 16>{});
 }
 
+// f(how many of its best a lane keeps in order and merges with other lanes', or 0 where the best of the lanes' first is taken k times instead).  32768 bf16 tokens, merged / taken one by one,
+// us: of 256 experts 4: 13.7 / 18.3, 8: 16.4 / 22.5, 16: 21.5 / 31.2; of 1000 experts 8: 71 / 87, 16: 98 / 120; with fewer experts to a lane of 128 4: 9.9 / 10.4, 6: 12.4 / 11.4,
+// 10: 16.0 / 13.3; of 512 8: 47 / 42.
+template <int L, int N, class F>
+static rtopk_status by_choices(std::integral_constant<int, L>, std::integral_constant<int, N>, int64_t k, F&& f) {
+    if constexpr (N == 16) {
+        if (k <= 4) return f(std::integral_constant<int, 4>{});
+        if (k <= 8) return f(std::integral_constant<int, 8>{});
+        if (L == 16 || k <= 16) return f(std::integral_constant<int, 16>{});
+    }
+    if constexpr (N != 16 || L != 16) return f(std::integral_constant<int, 0>{});
+    return RTOPK_ERR_INVALID_ARG;  // (16 lanes take 16 choices at most)
+}
+
 }  // namespace rtopk
 
 using namespace rtopk;
@@ -456,16 +579,17 @@ rtopk_status rtopk_route(const void* logits, int64_t tokens, int64_t experts, in
     (void)hipGetLastError();  // an error left by earlier HIP calls of the process is not this call's
     return by_type(dt, [&](auto t) {
         return by_experts(experts, k, [&](auto lanes, auto per_lane) {
-            constexpr int DT = decltype(t)::value, L = decltype(lanes)::value, N = decltype(per_lane)::value;
-            auto launch = [&](auto block, int64_t most) {
-                constexpr int B = decltype(block)::value;
-                const int64_t wgs = (tokens + B / L - 1) / (B / L);
-                hipLaunchKernelGGL((k_route<DT, L, N, B>), dim3((unsigned)(wgs < most ? wgs : most)), dim3(B), 0, (hipStream_t)hip_stream, P);
-            };
-            // Tokens are counted in LDS first.  Adds to one line of memory take 11 ns each, whoever makes them, so where they are counted few and large workgroups take all of them.
-            if (counts && tokens > 4096) launch(std::integral_constant<int, 1024>{}, 256);
-            else launch(std::integral_constant<int, 256>{}, 2048);
-            return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
+            return by_choices(lanes, per_lane, k, [&](auto most) {
+                constexpr int DT = decltype(t)::value, L = decltype(lanes)::value, N = decltype(per_lane)::value, K = decltype(most)::value;
+                // Tokens are counted in LDS first.  Adds to one line of memory take 11 ns each, whoever makes them, so where many are counted few and large workgroups take all of them.
+                const bool few = counts && tokens > 4096;
+                const int block = few ? kRouteBlock : 256, at_once = block / L;
+                const int64_t wgs = (tokens + at_once - 1) / at_once, most_wgs = few ? 256 : 2048;
+                const size_t lds = ((size_t)at_once * RouteShape<L, N>::kStage + (counts ? experts : 0)) * sizeof(u32);
+                if (lds > 65536) (void)hipFuncSetAttribute((const void*)k_route<DT, L, N, K>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                hipLaunchKernelGGL((k_route<DT, L, N, K>), dim3((unsigned)(wgs < most_wgs ? wgs : most_wgs)), dim3(block), lds, (hipStream_t)hip_stream, P);
+                return hipGetLastError() == hipSuccess ? RTOPK_OK : RTOPK_ERR_HIP;
+            });
         });
     });
 }
