@@ -62,43 +62,35 @@ __device__ __forceinline__ void wave_sync() {
 
 __device__ __forceinline__ float number_of_f32_key(u32 o) { return __uint_as_float((o & 0x80000000u) ? (o ^ 0x80000000u) : ~o); }
 
-// A lane's logits, -inf beyond the row.  `aligned`: rows start on a multiple of the lane's bytes, 16 at most; otherwise the token's lanes fetch neighbouring elements and change them
-// by way of `stage` (56182 tokens of 198 bf16 experts, both passes: 100 us with every lane fetching its own).
-template <int DT, int L, int N>
-__device__ __forceinline__ void lane_logits(const char* row, u32 l, u32 experts, bool aligned, float* stage, float (&x)[N]) {
+// Words of a lane's elements, wherever they start: the memory takes 4, 8 and 16 bytes from any element on.
+template <int BYTES> struct LaneWord;
+template <> struct LaneWord<4> { typedef u32 T __attribute__((aligned(2))); };
+template <> struct LaneWord<8> { typedef u32 T __attribute__((ext_vector_type(2), aligned(2))); };
+template <> struct LaneWord<16> { typedef u32 T __attribute__((ext_vector_type(4), aligned(2))); };
+
+// A lane's logits from `first` on, -inf beyond the row.  Words that lie in the row are fetched whole, also where rows are not on their grid, and the last one's elements one by one.
+template <int DT, int N>
+__device__ __forceinline__ void lane_logits(const char* row, u32 first, u32 experts, float (&x)[N]) {
     constexpr int kBytes = N * RowElem<DT>::kBytes, kWord = kBytes < 16 ? kBytes : 16;
-    const u32 first = l * N;
     if constexpr (kBytes >= 4) {
-        if (aligned) {
-            if (first + N <= experts) {
-                u32 w[kBytes / 4];
+        constexpr int E = kWord / RowElem<DT>::kBytes;
+        typedef typename LaneWord<kWord>::T Word;
 #pragma unroll
-                for (int i = 0; i < kBytes / kWord; ++i) {
-                    const char* p = row + (size_t)first * RowElem<DT>::kBytes + i * kWord;
-                    if constexpr (kWord == 16) *(u32x4*)&w[i * 4] = *(const u32x4*)p;
-                    else if constexpr (kWord == 8) *(uint2*)&w[0] = *(const uint2*)p;
-                    else w[0] = *(const u32*)p;
-                }
+        for (int i = 0; i < N / E; ++i) {
+            if (first + (i + 1) * E <= experts) {
+                u32 w[kWord / 4];
+                *(Word*)w = *(const Word*)(row + (size_t)first * RowElem<DT>::kBytes + i * kWord);
 #pragma unroll
-                for (int j = 0; j < N; ++j) x[j] = RowElem<DT>::from_bits(DT == RTOPK_F32 ? w[j] : (w[j / 2] >> (j & 1 ? 16 : 0)) & 0xffffu);
+                for (int j = 0; j < E; ++j) x[i * E + j] = RowElem<DT>::from_bits(DT == RTOPK_F32 ? w[j] : (w[j / 2] >> (j & 1 ? 16 : 0)) & 0xffffu);
             } else {
 #pragma unroll
-                for (int j = 0; j < N; ++j) x[j] = first + j < experts ? RowElem<DT>::load(row, first + j) : -__builtin_inff();
+                for (int j = 0; j < E; ++j) x[i * E + j] = first + i * E + j < experts ? RowElem<DT>::load(row, first + i * E + j) : -__builtin_inff();
             }
-            return;
         }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = first + j < experts ? RowElem<DT>::load(row, first + j) : -__builtin_inff();
     }
-    typedef RouteShape<L, N> S;
-    wave_sync();  // (what the stage held has been read)
-    float t[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) t[j] = j * L + l < experts ? RowElem<DT>::load(row, j * L + l) : -__builtin_inff();
-#pragma unroll
-    for (int j = 0; j < N; ++j) stage[S::place(j * L + l)] = t[j];
-    wave_sync();
-#pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = stage[S::place(first + j)];
-    wave_sync();
 }
 
 // 1 / d and a / d as a division rounds them (Markstein's theorem: a reciprocal that is off by one unit, put right by its residual, is the rounded one, and so is a quotient put right
@@ -273,8 +265,6 @@ __global__ void __launch_bounds__(kRouteBlock) k_route(RouteParams P) {
     u32* const tally = (u32*)(stage + B / L * S::kStage);  // what this workgroup's tokens chose
     const u32 lane = lane_id(), slot = threadIdx.x / L;
     const bool sigmoid = (P.flags & RTOPK_ROUTE_SIGMOID) != 0, top2 = (P.flags & RTOPK_ROUTE_GROUP_TOP2) != 0;
-    constexpr u32 kWord = N * RowElem<DT>::kBytes < 16 ? N * RowElem<DT>::kBytes : 16, kBiasWord = N * 4 < 16 ? N * 4 : 16;
-    const bool aligned = (((uintptr_t)P.logits | (uintptr_t)P.row_bytes) & (kWord - 1)) == 0;
     // groups of whole lanes, as many as a power of two: their best two are found on the way across those lanes
     const u32 group_lanes = P.group_size / N;
     const bool by_lanes = group_lanes * N == P.group_size && (group_lanes & (group_lanes - 1)) == 0 && group_lanes <= 16;
@@ -289,8 +279,8 @@ __global__ void __launch_bounds__(kRouteBlock) k_route(RouteParams P) {
         u32 l = lane % L;
         asm volatile("" : "+v"(l));  // (what depends on the lane alone is made anew for every token: kept, it takes more registers than there are)
         float x[N], s[N], bias[N];
-        lane_logits<DT, L, N>(P.logits + row * P.row_bytes, l, P.experts, aligned, mine, x);
-        if (P.bias) lane_logits<RTOPK_F32, L, N>((const char*)P.bias, l, P.experts, ((uintptr_t)P.bias & (kBiasWord - 1)) == 0, mine, bias);
+        lane_logits<DT, N>(P.logits + row * P.row_bytes, l * N, P.experts, x);
+        if (P.bias) lane_logits<RTOPK_F32, N>((const char*)P.bias, l * N, P.experts, bias);
         scores_of<L, N>(x, s, sigmoid);
         u32 key[N];  // orders the choice; 0 for what may not be chosen
 #pragma unroll
@@ -445,8 +435,6 @@ __global__ void __launch_bounds__(kRouteGradBlock) k_route_grad(RouteParams P) {
     __shared__ float stage[kRouteGradBlock / L][S::kStage];
     const u32 lane = lane_id(), l = lane % L, slot = threadIdx.x / L;
     const bool sigmoid = (P.flags & RTOPK_ROUTE_SIGMOID) != 0, renormalize = (P.flags & RTOPK_ROUTE_RENORMALIZE) != 0;
-    constexpr u32 kWord = N * RowElem<DT>::kBytes < 16 ? N * RowElem<DT>::kBytes : 16;
-    const bool aligned = (((uintptr_t)P.logits | (uintptr_t)P.row_bytes) & (kWord - 1)) == 0, aligned_out = (((uintptr_t)P.grad | (uintptr_t)P.grad_bytes) & (kWord - 1)) == 0;
     float* const mine = stage[slot];
     for (long long first = (long long)blockIdx.x * (kRouteGradBlock / L); first < P.tokens; first += (long long)gridDim.x * (kRouteGradBlock / L)) {
         const long long token = first + slot, row = token < P.tokens ? token : P.tokens - 1;
@@ -454,7 +442,7 @@ __global__ void __launch_bounds__(kRouteGradBlock) k_route_grad(RouteParams P) {
         const bool there = e >= 0 && e < (long long)P.experts;
         float g = there ? P.scale * P.grad_weights[row * P.k + l] : 0.0f;
         float x[N], s[N];
-        lane_logits<DT, L, N>(P.logits + row * P.row_bytes, l, P.experts, aligned, mine, x);
+        lane_logits<DT, N>(P.logits + row * P.row_bytes, l * N, P.experts, x);
         scores_of<L, N>(x, s, sigmoid);
         wave_sync();  // (the last tokens' sums have been read)
 #pragma unroll
@@ -476,31 +464,28 @@ __global__ void __launch_bounds__(kRouteGradBlock) k_route_grad(RouteParams P) {
         wave_sync();
         if (token < P.tokens) {
             char* out = P.grad + row * P.grad_bytes;
-            constexpr int kBytes = N * RowElem<DT>::kBytes;
+            constexpr int kBytes = N * RowElem<DT>::kBytes, kWord = kBytes < 16 ? kBytes : 16;
             if constexpr (kBytes >= 4) {
-                if (aligned_out && l * N + N <= P.experts) {
-                    u32 w[kBytes / 4];
+                constexpr int E = kWord / RowElem<DT>::kBytes;
+                typedef typename LaneWord<kWord>::T Word;
 #pragma unroll
-                    for (int j = 0; j < N; j += DT == RTOPK_F32 ? 1 : 2) {
-                        const float a = mine[S::place(l * N + j)], b = DT == RTOPK_F32 ? 0.0f : mine[S::place(l * N + j + 1)];
-                        if constexpr (DT == RTOPK_F32) w[j] = __float_as_uint(a);
-                        else w[j / 2] = RowElem<DT>::pack2(a, b);
-                    }
+                for (int i = 0; i < N / E; ++i) {
+                    const u32 from = l * N + i * E;
+                    if (from + E <= P.experts) {
+                        u32 w[kWord / 4];
 #pragma unroll
-                    for (int i = 0; i < kBytes / (int)kWord; ++i) {
-                        char* p = out + (size_t)l * kBytes + i * kWord;
-                        if constexpr (kWord == 16) *(u32x4*)p = *(const u32x4*)&w[i * 4];
-                        else if constexpr (kWord == 8) *(uint2*)p = *(const uint2*)&w[0];
-                        else *(u32*)p = w[0];
+                        for (int j = 0; j < kWord / 4; ++j) {
+                            if constexpr (DT == RTOPK_F32) w[j] = __float_as_uint(mine[S::place(from + j)]);
+                            else w[j] = RowElem<DT>::pack2(mine[S::place(from + 2 * j)], mine[S::place(from + 2 * j + 1)]);
+                        }
+                        *(Word*)(out + (size_t)from * RowElem<DT>::kBytes) = *(const Word*)w;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < E; ++j)
+                            if (from + j < P.experts) RowElem<DT>::store(out, from + j, mine[S::place(from + j)]);
                     }
                 }
-            }
-            // (lanes that hold the row's last ones, and rows that are not aligned: neighbouring elements at a time)
-            if (!aligned_out || kBytes < 4) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (j * L + l < P.experts) RowElem<DT>::store(out, j * L + l, mine[S::place(j * L + l)]);
-            } else if (l * N + N > P.experts) {
+            } else {
 #pragma unroll
                 for (int j = 0; j < N; ++j)
                     if (l * N + j < P.experts) RowElem<DT>::store(out, l * N + j, mine[S::place(l * N + j)]);
