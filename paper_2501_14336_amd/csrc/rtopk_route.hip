@@ -344,11 +344,12 @@ __global__ void __launch_bounds__(kRouteBlock) k_route(RouteParams P) {
             for (u32 g = 0; g < P.groups; ++g) {
                 const u32 o = ((const u32*)mine)[g];
 #pragma unroll
-                for (int t = 0; t < 64 / L; ++t) better[t] += o > value[t] || (o == value[t] && g < l + t * L);
+                for (int t = 0; t < 64 / L; ++t)
+                    if (t * L < P.groups) better[t] += o > value[t] || (o == value[t] && g < l + t * L);
             }
             u64 stays = 0;
 #pragma unroll
-            for (int t = 0; t < 64 / L; ++t) {
+            for (int t = 0; t < 64 / L && t * L < P.groups; ++t) {
                 const u64 b = ballot64(l + t * L < P.groups && better[t] < P.topk_groups) >> (lane - l);
                 stays |= (L == 64 ? b : b & ((1ull << (L % 64)) - 1)) << (t * L % 64);
             }
