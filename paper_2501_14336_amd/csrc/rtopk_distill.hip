@@ -182,7 +182,14 @@ static int64_t vectors_of(const void* x, int64_t n, int64_t stride, rtopk_dtype 
     const bool even = (uintptr_t)x % 16 == 0 && stride % E == 0;
     return (n + (even ? 0 : E - 1) + E - 1) / E;
 }
-static bool step_is_held(int64_t batch, int64_t vecs) { return vecs <= kHeldVecs && (batch >= 128 || vecs <= 4096); }
+// Whether workgroups keep their rows from the loss to the gradient.  Rows of more than 8192 vectors take a compute unit each, so a batch takes as long as the next multiple of 256: kept where
+// it nearly is one (kept / in two launches, us, rows of 131072 bf16 with the rest: 257 rows 70 / 48, 400 71 / 66, 512 74 / 81, 600 103 / 95, 900 135 / 131, 1030 167 / 148).
+// Of shorter ones several share a unit (rows of 65536: 130 rows 21 / 23, 257 30 / 32, 600 46 / 52).
+static bool step_is_held(int64_t batch, int64_t vecs) {
+    if (vecs <= 4096) return true;
+    if (vecs <= 8192) return batch >= 128;
+    return vecs <= kHeldVecs && batch * 10 >= (batch + 255) / 256 * 256 * 9;
+}
 
 }  // namespace rtopk
 

@@ -96,6 +96,15 @@ def test_distill_rows_that_a_workgroup_keeps(batch, vectors, dtype, odd, tail):
 
 
 @pytest.mark.parametrize("tail", [False, True], ids=["list", "rest"])
+@pytest.mark.parametrize("batch,vectors,dtype,odd", [
+    (256, 16384, torch.bfloat16, 0), (505, 10000, torch.float16, 0), (250, 16383, torch.bfloat16, 5), (480, 20480, torch.float32, 0), (236, 20479, torch.float16, 7),
+    (768, 8200, torch.float32, 0), (257, 16384, torch.bfloat16, 0)])
+def test_distill_rows_that_fill_the_compute_units(batch, vectors, dtype, odd, tail):
+    n = vectors * (4 if dtype is torch.float32 else 8)
+    _check_step(_rows(batch, n - odd, dtype, batch + n, lead=odd, apart=odd), 70, tail, 0.8)
+
+
+@pytest.mark.parametrize("tail", [False, True], ids=["list", "rest"])
 @pytest.mark.parametrize("batch,n,k", [(260, 9000, 1025), (130, 70000, 2500), (3, 30000, 5000), (2, 200000, 2049), (500, 2600, 2600)])
 def test_distill_lists_longer_than_the_entries_that_threads_keep(batch, n, k, tail):
     _check_step(_rows(batch, n, torch.bfloat16, k), k, tail, 1.0, torch.float16)
