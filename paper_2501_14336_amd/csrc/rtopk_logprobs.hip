@@ -48,21 +48,27 @@ __device__ __forceinline__ u32 key_of(float x) { return KeyOf<RTOPK_F32>::key(__
 __device__ __forceinline__ float number_of(u32 key) { return __uint_as_float((key & 0x80000000u) ? (key ^ 0x80000000u) : ~key); }  // (the key of all NaNs gives one)
 __device__ __forceinline__ u64 entry_of(u32 key, u32 col) { return ((u64)key << 32) | (u32)~col; }
 
-// A bound that at least `want` (up to 64) of the workgroup's threads' values are not below; 0 where `threads`, the first so many that have one, do not fill a wave.  `sm` has an entry
+// A bound that at least `want` (up to 64) of the workgroup's threads' keys are not below; 0 where `threads`, the first so many that have one, do not fill a wave.  `sm` has an entry
 // per wave and is free after the next barrier.
-template <int B, class T>
-__device__ __forceinline__ T bound_of_threads(T v, u32 threads, u32 want, T* sm) {
+template <int B>
+__device__ __forceinline__ u32 bound_of_threads(u32 v, u32 threads, u32 want, u32* sm) {
     const u32 waves = min(threads, (u32)B) / 64;  // full ones: the rest may hold anything
     const u32 of_wave = waves == 0 ? 0 : (want + waves - 1) / waves;
-    T best = 0;
-    for (u32 i = 0; i < of_wave; ++i) {
+    u32 best = 0;
+    for (u32 found = 0; found < of_wave;) {  // the wave's of_wave-th largest, or one equal to it
         best = wave_largest(v);
-        const u64 who = ballot64(v == best);
-        if (lane_id() == (u32)__builtin_ctzll(who)) v = 0;
+        found += (u32)__builtin_popcountll(ballot64(v == best));
+        v = v == best ? 0u : v;
     }
     if (lane_id() == 0) sm[threadIdx.x >> 6] = best;
     __syncthreads();
-    return waves == 0 ? (T)0 : wave_smallest(sm[lane_id() % (B / 64) < waves ? lane_id() % (B / 64) : 0]);
+    if (waves == 0) return 0;
+    const u32 mine = sm[lane_id() % (B / 64) < waves ? lane_id() % (B / 64) : 0], enough = (want + of_wave - 1) / of_wave;
+    if (enough == waves) return wave_smallest(mine);
+    u32 not_below = 0;  // of so many waves as it takes, the best ones
+#pragma unroll
+    for (u32 w = 0; w < B / 64; ++w) not_below += w < waves && (u32)__builtin_amdgcn_readlane((int)mine, (int)w) >= mine;
+    return wave_largest(not_below >= enough ? mine : 0u);
 }
 
 template <int B>
@@ -217,12 +223,18 @@ __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
     }
     auto list_vector = [&](u32 v, const float (&x)[E]) {
         if constexpr (TOP) {
+            u32 which = 0;
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const u32 col = v * E + j - r.lead;
-                if (!(x[j] < bound_number) && col < r.n && key_of(x[j]) >= bound) {
+            for (int j = 0; j < E; ++j) which |= !(x[j] < bound_number) ? 1u << j : 0u;
+            while (which) {  // (one, mostly)
+                const u32 j = (u32)__builtin_ctz(which), col = v * E + j - r.lead;
+                which &= which - 1;
+                float y = x[0];
+#pragma unroll
+                for (int i = 1; i < E; ++i) y = j == (u32)i ? x[i] : y;
+                if (col < r.n && key_of(y) >= bound) {
                     const u32 place = atomicAdd(&top.count, 1u);
-                    if (place < kListRoom) top.list[place] = entry_of(key_of(x[j]), col);
+                    if (place < kListRoom) top.list[place] = entry_of(key_of(y), col);
                 }
             }
         }
