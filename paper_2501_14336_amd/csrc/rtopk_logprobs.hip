@@ -32,7 +32,7 @@ __device__ __forceinline__ float logprob_of(float x, float m, float s, float ln_
 // The k best of a sweep (k up to 64), on the way.  Elements are entries: the key of the number, NaN above all, above the complement of the column, so that all differ and the
 // larger is the better one.
 //
-// A lane keeps its running maximum for the softmax anyway.  Of the lane maxima of W waves that are full, the smallest of the waves' (k / W)-th largest has at least k elements that are not below it: a
+// A lane keeps its running maximum for the softmax anyway.  Of the lane maxima of groups of lanes, the r-th largest of each group has r elements that are not below it, and the (k / r)-th best of those has k: a
 // bound of the k-th best.  One is taken after the first tile; from then on a lane notes the vectors whose maximum is not below it, a bit each.  Another, from
 // all the lanes have seen, is taken at the end, and only what was noted by lanes whose maximum is not below that is fetched again: of data in no order about twice k vectors, of which about
 // as many elements are listed and ranked by comparing each with all others.  A list too long for LDS (equal elements, or the best in few lanes) leads to a radix selection of the
@@ -48,35 +48,55 @@ __device__ __forceinline__ u32 key_of(float x) { return KeyOf<RTOPK_F32>::key(__
 __device__ __forceinline__ float number_of(u32 key) { return __uint_as_float((key & 0x80000000u) ? (key ^ 0x80000000u) : ~key); }  // (the key of all NaNs gives one)
 __device__ __forceinline__ u64 entry_of(u32 key, u32 col) { return ((u64)key << 32) | (u32)~col; }
 
-// A bound that at least `want` (up to 64) of the workgroup's threads' keys are not below; 0 where `threads`, the first so many that have one, do not fill a wave.  `sm` has an entry
-// per wave and is free after the next barrier.
+constexpr int kBoundGroups = 16;  // of a workgroup's threads
+
+// The largest of a group of GL lanes, in all of them.
+template <int GL>
+__device__ __forceinline__ u32 group_largest(u32 v) {
+    auto turned = [](auto ctrl, u32 v) { return (u32)__builtin_amdgcn_update_dpp((int)v, (int)v, decltype(ctrl)::value, 0xf, 0xf, false); };
+    v = max(v, turned(std::integral_constant<int, 0x128>{}, v));
+    v = max(v, turned(std::integral_constant<int, 0x124>{}, v));
+    v = max(v, turned(std::integral_constant<int, 0x122>{}, v));
+    v = max(v, turned(std::integral_constant<int, 0x121>{}, v));
+    if constexpr (GL >= 32) {
+        const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max(rows[0], rows[1]);
+    }
+    if constexpr (GL >= 64) {
+        const auto halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = max(halves[0], halves[1]);
+    }
+    return v;
+}
+
+// A bound that at least `want` of the workgroup's threads' keys are not below; 0 where it finds none.  `threads`: the first so many that have one.  `sm` has an entry per group and is free after
+// the next barrier.
 template <int B>
 __device__ __forceinline__ u32 bound_of_threads(u32 v, u32 threads, u32 want, u32* sm) {
-    const u32 waves = min(threads, (u32)B) / 64;  // full ones: the rest may hold anything
-    const u32 of_wave = waves == 0 ? 0 : (want + waves - 1) / waves;
+    constexpr u32 kLanes = B / kBoundGroups;
+    const u32 groups = max(min(threads, (u32)B) / kLanes, 1u);  // full ones: the rest may hold anything
+    const u32 least = (want + groups - 1) / groups, each = least + (least > 1 ? 1u : 0u);
+    // (a round more than it takes, and fewer groups: 32 of 2853 rows of 5808 bf16 21.1 us, without 23.8)
     u32 best = 0;
-    for (u32 found = 0; found < of_wave;) {  // the wave's of_wave-th largest, or one equal to it
-        best = wave_largest(v);
-        found += (u32)__builtin_popcountll(ballot64(v == best));
+    for (u32 i = 0; i < each; ++i) {  // what at least so many of the group's lanes are not below
+        best = group_largest<kLanes>(v);
         v = v == best ? 0u : v;
     }
-    if (lane_id() == 0) sm[threadIdx.x >> 6] = best;
+    if (threadIdx.x % kLanes == 0) sm[threadIdx.x / kLanes] = threads < kLanes ? 0u : best;
     __syncthreads();
-    if (waves == 0) return 0;
-    const u32 mine = sm[lane_id() % (B / 64) < waves ? lane_id() % (B / 64) : 0], enough = (want + of_wave - 1) / of_wave;
-    if (enough == waves) return wave_smallest(mine);
-    u32 not_below = 0;  // of so many waves as it takes, the best ones
+    const u32 g = lane_id() % kBoundGroups, mine = g < groups ? sm[g] : 0u, enough = (want + each - 1) / each;
+    u32 not_below = 0;  // of so many groups as it takes, the best ones
 #pragma unroll
-    for (u32 w = 0; w < B / 64; ++w) not_below += w < waves && (u32)__builtin_amdgcn_readlane((int)mine, (int)w) >= mine;
-    return wave_largest(not_below >= enough ? mine : 0u);
+    for (int i = 0; i < kBoundGroups; ++i) not_below += (u32)__builtin_amdgcn_readlane((int)mine, i) >= mine;
+    return group_largest<kBoundGroups>(not_below >= enough ? mine : 0u);
 }
 
 template <int B>
 struct TopShared {
     u64 list[kListRoom];
     u32 hist[256];
-    u64 bound64[B / 64];
-    u32 bound[B / 64];
+    u64 bound64;
+    u32 bound[2][kBoundGroups];
     u32 count, digit, above, scan[B / 64];
 };
 
@@ -195,8 +215,8 @@ __device__ __forceinline__ void write_top(const LogprobsParams& P, long long row
 struct NoTop {};
 
 // The one pass over a row, by a workgroup that then has its results, or, where there are few rows, by several that leave their parts to k_logprobs_finish.  Bound by memory where there is
-// much of it: 1024 rows of 131072 bf16, scored with their entropy, 48 us or 5.6 TB/s; 512 rows of 100003 fp16 24 us, 4.3 TB/s; 300 rows of 50257 fp32 with 5 alternatives 17.2 us,
-// 3.5 TB/s (each compute unit has a row or two: the second does not fill them).  One row of 131072 bf16 with 20 alternatives: 6.6 us, as long as 16 of them, a wave's way from its
+// much of it: 1024 rows of 131072 bf16, scored with their entropy, 48 us or 5.6 TB/s; 512 rows of 100003 fp16 24 us, 4.3 TB/s; 300 rows of 50257 fp32 with 5 alternatives 16.6 us,
+// 3.6 TB/s (each compute unit has a row or two: the second does not fill them).  One row of 131072 bf16 with 20 alternatives: 6.0 us, as long as 16 of them, a wave's way from its
 // loads to what it lists.  16-bit logits come within a fifth of the rate of 2^x, a quarter of that of sums.
 template <int DT, int B, int V, bool NT, bool W, bool TOP, bool WHOLE>
 __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
@@ -253,7 +273,7 @@ __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
         soft_add_to<W>(a, x, t, P.c);
         if constexpr (TOP) {
             if (first == v0) {
-                bound = bound_of_threads<B>(key_of(a.m), v1 - v0, (u32)P.k, top.bound);
+                bound = bound_of_threads<B>(key_of(a.m), v1 - v0, (u32)P.k, top.bound[0]);
                 bound_number = bound == 0 ? -__builtin_inff() : number_of(bound);
             }
             u32 hits = 0;
@@ -282,7 +302,7 @@ __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
         const long long here = (long long)min((u64)v1 * E, (u64)r.lead + r.n) - (long long)max((u64)v0 * E, (u64)r.lead);  // columns
         const u32 want = here < P.k ? (here < 0 ? 0u : (u32)here) : (u32)P.k;
         if (!one_tile) {
-            bound = max(bound, bound_of_threads<B>(key_of(mine), B, (u32)P.k, (u32*)top.bound64));
+            bound = max(bound, bound_of_threads<B>(key_of(mine), B, (u32)P.k, top.bound[1]));
             bound_number = bound == 0 ? -__builtin_inff() : number_of(bound);
             if (!(mine < bound_number)) {
                 while (noted) {
@@ -376,14 +396,14 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
         const u64 mine = by_heads ? head : best;
         const u32 others = by_heads ? P.parts : kFinishBlock;
         top.list[threadIdx.x] = mine;
-        if (threadIdx.x == 0) top.bound64[0] = 0;
+        if (threadIdx.x == 0) top.bound64 = 0;
         __syncthreads();
         u32 rank = 0;
 #pragma unroll 16
         for (u32 j = 0; j < others; ++j) rank += top.list[j] > mine;
-        if (rank == (u32)P.k - 1 && mine != 0 && threadIdx.x < others) top.bound64[0] = mine;
+        if (rank == (u32)P.k - 1 && mine != 0 && threadIdx.x < others) top.bound64 = mine;
         __syncthreads();
-        const u64 bound = top.bound64[0];
+        const u64 bound = top.bound64;
 #pragma unroll
         for (int j = 0; j < kEach; ++j)
             if (e[j] >= bound && e[j] != 0) {
