@@ -10,10 +10,37 @@
 
 namespace rtopk {
 
+// A row's list; the thread's first entry is fetched when the kernel begins, three trips that the row's hide.
+template <int DT>
+struct RowList {
+    struct Entry {
+        long long t;
+        float z, x;  // the teacher's and the student's logit
+    };
+    const DistillParams& P;
+    const RowView<DT>& r;
+    long long from;
+    Entry first;
+    __device__ __forceinline__ RowList(const DistillParams& P, long long row, const RowView<DT>& r) : P(P), r(r), from(row * P.k) {
+        first = {-1, 0.0f, 0.0f};
+        if ((long long)threadIdx.x < P.k) first = entry(threadIdx.x);
+    }
+    __device__ __forceinline__ Entry entry(long long i) const {
+        Entry e = {P.columns[from + i], load_as_float(P.values, P.value_dt, (size_t)(from + i)), 0.0f};
+        if (e.t >= 0 && e.t < (long long)P.n) e.x = RowElem<DT>::load(r.x, (u32)e.t);
+        return e;
+    }
+    // f(entry, whether it is the first) for the thread's ones
+    template <int B, class F>
+    __device__ __forceinline__ void each(F&& f) const {
+        if ((long long)threadIdx.x < P.k) f(first, true);
+        for (long long i = (long long)threadIdx.x + B; i < P.k; i += B) f(entry(i), false);
+    }
+};
+
 // The loss of a row, and what its gradient needs of it, from the sums of its columns (TAIL: of those that are not listed, and of those that are).
 template <int DT, bool TAIL, int B>
-__device__ __forceinline__ void loss_of_row(const DistillParams& P, long long row, const RowView<DT>& r, SoftSum a, const SoftSum& listed, float4* sm, double* sums) {
-    const long long* columns = P.columns + row * P.k;
+__device__ __forceinline__ void loss_of_row(const DistillParams& P, long long row, const RowList<DT>& list, SoftSum a, const SoftSum& listed, float4* sm, double* sums) {
     const SoftSum others = a;
     if (TAIL) a = soft_join<false>(a, listed, P.c);
     DistillRow d;
@@ -23,11 +50,12 @@ __device__ __forceinline__ void loss_of_row(const DistillParams& P, long long ro
         d.zmul = 1.0f;
     } else {
         SoftSum z;
-        for (long long i = threadIdx.x; i < P.k; i += B)
-            if (columns[i] >= 0) {
-                const float v[1] = {load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i))};
+        list.template each<B>([&](auto e, bool) {
+            if (e.t >= 0) {
+                const float v[1] = {e.z};
                 soft_add<false>(z, v, P.c);
             }
+        });
         z = soft_block<B, false>(z, P.c, sm);
         zs = z.s;
         d.zref = finite_or_zero(z.m);
@@ -37,18 +65,13 @@ __device__ __forceinline__ void loss_of_row(const DistillParams& P, long long ro
     const float ln_s = kLn2 * log2_fast(a.s);
     float loss = 0.0f;
     double share = 0.0;
-    for (long long i = threadIdx.x; i < P.k; i += B) {
-        const long long t = columns[i];
-        if (t < 0) continue;
-        const float z = load_as_float(P.values, P.value_dt, (size_t)(row * P.k + i)), lq = ln_share(z, d, TAIL, ln_zmul, P.inv_t), qi = expf(lq);
-        if (TAIL) share += exact_share(z, d.zref, P.inv_t);
-        if (t >= (long long)P.n) {
-            loss += __builtin_nanf("");
-        } else if (qi != 0.0f) {
-            const float x = RowElem<DT>::load(r.x, (u32)t);
-            loss += qi * (lq - (a.s == 0.0f ? -__builtin_inff() : (x - a.m) * P.inv_t - ln_s));
-        }
-    }
+    list.template each<B>([&](auto e, bool) {
+        if (e.t < 0) return;
+        const float lq = ln_share(e.z, d, TAIL, ln_zmul, P.inv_t), qi = expf(lq);
+        if (TAIL) share += exact_share(e.z, d.zref, P.inv_t);
+        if (e.t >= (long long)P.n) loss += __builtin_nanf("");
+        else if (qi != 0.0f) loss += qi * (lq - (a.s == 0.0f ? -__builtin_inff() : (e.x - a.m) * P.inv_t - ln_s));
+    });
     loss = sum_block<B>(loss, (float*)sums);
     if (TAIL) share = sum_block<B>(share, sums + B / 64);
     loss += finish_row<TAIL>(d, a, others, share, zs, P);
@@ -61,7 +84,7 @@ __device__ __forceinline__ void loss_of_row(const DistillParams& P, long long ro
 constexpr int kDistillVecs = 4;
 
 // Statistics of a row, or of a part of one; TAIL: apart for columns that are listed and for the others.  WHOLE: of the row, and its loss.  One reading of the row: 200 rows of 50257 fp32 with
-// the rest, lists of 50: 13.7 us, 2.9 TB/s from 200 compute units, each of which reads its row, adds it up and waits for the row's list at the end.  8 rows of 30011 fp16 with lists of 100:
+// the rest, lists of 50: 12.6 us, 3.2 TB/s from 200 compute units, one row each.  8 rows of 30011 fp16 with lists of 100:
 // 6.1 us, the way of one workgroup.
 template <int DT, bool NT, bool TAIL, int B, bool WHOLE>
 __global__ void __launch_bounds__(B) k_distill_part(DistillParams P) {
@@ -73,25 +96,31 @@ __global__ void __launch_bounds__(B) k_distill_part(DistillParams P) {
     const long long row = P.row0 + (WHOLE ? blockIdx.x : blockIdx.x / P.parts);
     const RowView<DT> r(P.student, row, P.row_bytes, P.n);
     const u32 v0 = part * P.part_vecs, v1 = part_end(v0, P.part_vecs, r.nvec);
+    const RowList<DT> list(P, row, r);
     SoftSum a, listed;
+    bool first_counts = false;
     if (TAIL) {
-        const long long* columns = P.columns + row * P.k;
         for (u32 i = threadIdx.x; i < (P.part_vecs + 3) / 4; i += B) marks[i] = 0;
-        __syncthreads();
-        for (long long i = threadIdx.x; i < P.k; i += B) {
-            const long long t = columns[i];
-            const u64 p = (u64)t + r.lead - (u64)v0 * E;  // (wraps below the part)
-            if (t >= 0 && t < (long long)P.n && p < (u64)(v1 - v0) * E) {
-                const u32 v = (u32)p / E, bit = 1u << ((v & 3) * 8 + (u32)p % E);
-                if (!(atomicOr(&marks[v >> 2], bit) & bit)) {  // a column listed twice counts once
-                    const float x[1] = {RowElem<DT>::load(r.x, (u32)t)};
-                    soft_add<false>(listed, x, P.c);
-                }
-            }
-        }
-        __syncthreads();
     }
     sweep_vectors<DT, B, V, NT>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
+        if (TAIL && first == v0) {  // (with the first two tiles on their way)
+            __syncthreads();
+            list.template each<B>([&](auto e, bool is_first) {
+                const u64 p = (u64)e.t + r.lead - (u64)v0 * E;  // (wraps below the part)
+                if (e.t >= 0 && e.t < (long long)P.n && p < (u64)(v1 - v0) * E) {
+                    const u32 v = (u32)p / E, bit = 1u << ((v & 3) * 8 + (u32)p % E);
+                    if (!(atomicOr(&marks[v >> 2], bit) & bit)) {  // a column listed twice counts once
+                        if (is_first) {
+                            first_counts = true;
+                        } else {
+                            const float x[1] = {e.x};
+                            soft_add<false>(listed, x, P.c);
+                        }
+                    }
+                }
+            });
+            __syncthreads();
+        }
         float x[V * E];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -107,10 +136,14 @@ __global__ void __launch_bounds__(B) k_distill_part(DistillParams P) {
         }
         soft_add<false>(a, x, P.c);
     });
+    if (first_counts) {
+        const float x[1] = {list.first.x};
+        soft_add<false>(listed, x, P.c);
+    }
     a = soft_block<B, false>(a, P.c, sm[0]);
     if (TAIL) listed = soft_block<B, false>(listed, P.c, sm[1]);
     if (WHOLE) {
-        loss_of_row<DT, TAIL, B>(P, row, r, a, listed, sm[2], sums);
+        loss_of_row<DT, TAIL, B>(P, row, list, a, listed, sm[2], sums);
     } else if (threadIdx.x == 0) {
         P.partial[(row * P.parts + part) * 2] = packed(a);
         if (TAIL) P.partial[(row * P.parts + part) * 2 + 1] = packed(listed);
@@ -126,6 +159,7 @@ __global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams
     __shared__ double sums[2 * kDistillFinish / 64];
     const long long row = P.row0 + blockIdx.x;
     const RowView<DT> r(P.student, row, P.row_bytes, P.n);
+    const RowList<DT> list(P, row, r);
     SoftSum a, listed;
     for (u32 i = threadIdx.x; i < P.parts; i += kDistillFinish) {
         a = soft_join<false>(a, unpacked(P.partial[(row * P.parts + i) * 2]), P.c);
@@ -133,7 +167,7 @@ __global__ void __launch_bounds__(kDistillFinish) k_distill_finish(DistillParams
     }
     a = soft_block<kDistillFinish, false>(a, P.c, sm[0]);
     if (TAIL) listed = soft_block<kDistillFinish, false>(listed, P.c, sm[1]);
-    loss_of_row<DT, TAIL, kDistillFinish>(P, row, r, a, listed, sm[2], sums);
+    loss_of_row<DT, TAIL, kDistillFinish>(P, row, list, a, listed, sm[2], sums);
 }
 
 constexpr int kDistillGradBlock = 256, kDistillGradVecs = 2;
