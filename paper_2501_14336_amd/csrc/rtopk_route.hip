@@ -25,7 +25,8 @@ struct RouteParams {
 };
 
 // A token is taken by L lanes of a wave, lane l of them holding experts l N to l N + N - 1: 16 lanes up to 256 experts (four tokens to a wave: its steps across lanes are
-// moves within a row of 16, and cost the same for four tokens as for one), a whole wave beyond, or where more than 16 experts are wanted.
+// moves within a row of 16, and cost the same for four tokens as for one), 32 up to 512 (32768 tokens of 512 bf16 experts, 8 of them: 31.8 us, with a wave 42), a whole wave beyond, or where
+// more than 16 experts are wanted.
 template <int L, int N>
 struct RouteShape {
     static constexpr int kTokens = 64 / L;                    // of a wave
@@ -36,6 +37,12 @@ struct RouteShape {
 // Over a token's lanes, the same in all of them: rotations within rows of 16 lanes pair the same two sums in every lane.
 template <int CTRL>
 __device__ __forceinline__ u32 row_rotated(u32 v) { return (u32)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false); }
+// A wave's rows of 16 lanes in pairs (ROWS 1), or its halves (2): what the first of the pair has, and what the second has, in all lanes of both.
+template <int ROWS>
+__device__ __forceinline__ auto rows_of(u32 v) {
+    if constexpr (ROWS == 1) return __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    else return __builtin_amdgcn_permlane32_swap(v, v, false, false);
+}
 template <int L, class T, class Op>
 __device__ __forceinline__ T token_reduce(T v, Op&& op) {
     auto bits = [](T x) { return __builtin_bit_cast(u32, x); };
@@ -44,9 +51,13 @@ __device__ __forceinline__ T token_reduce(T v, Op&& op) {
     v = op(v, back(row_rotated<0x124>(bits(v))));
     v = op(v, back(row_rotated<0x122>(bits(v))));
     v = op(v, back(row_rotated<0x121>(bits(v))));
+    if constexpr (L >= 32) {
+        const auto pair = rows_of<1>(bits(v));
+        v = op(back(pair[0]), back(pair[1]));
+    }
     if constexpr (L == 64) {
-        v = op(v, __shfl_xor(v, 16));
-        v = op(v, __shfl_xor(v, 32));
+        const auto half = rows_of<2>(bits(v));
+        v = op(back(half[0]), back(half[1]));
     }
     return v;
 }
@@ -226,11 +237,7 @@ __device__ __forceinline__ void merge_rows(double* c) {
 #pragma unroll
     for (int i = 0; i < K; ++i) {
         const u64 v = __builtin_bit_cast(u64, c[i]);
-        auto swapped = [](u32 w) {
-            if constexpr (ROWS == 1) return __builtin_amdgcn_permlane16_swap(w, w, false, false);
-            else return __builtin_amdgcn_permlane32_swap(w, w, false, false);
-        };
-        const auto low = swapped((u32)v), high = swapped((u32)(v >> 32));
+        const auto low = rows_of<ROWS>((u32)v), high = rows_of<ROWS>((u32)(v >> 32));
         c[i] = choice_from(low[0], high[0]);
         b[i] = choice_from(low[1], high[1]);
     }
@@ -242,10 +249,8 @@ __device__ __forceinline__ void best_of_token(double* c) {
     merge_lanes<0x4e, K>(c);
     merge_lanes<0x141, K>(c);
     merge_lanes<0x140, K>(c);
-    if constexpr (L == 64) {
-        merge_rows<1, K>(c);
-        merge_rows<2, K>(c);
-    }
+    if constexpr (L >= 32) merge_rows<1, K>(c);
+    if constexpr (L == 64) merge_rows<2, K>(c);
 }
 
 // The two best keys of two sets.
@@ -255,7 +260,7 @@ __device__ __forceinline__ void best_two(u32& a, u32& b, u32 a2, u32 b2) {
 }
 
 // Bound by instructions: for 256 experts to 16 lanes about 1700 a wave of four tokens, most of them for the scores (2^x and the reciprocal at a quarter of the rate), the keys and the order.
-// 16384 tokens of 256 bf16 experts, 8 of 4 of 8 groups, with a bias: 11.9 us, and 17.2 with the counts, whose adds to a few lines of memory come at the end of all workgroups at once.
+// 16384 tokens of 256 bf16 experts, 8 of 4 of 8 groups, with a bias: 11.9 us, and 17.0 with the counts, whose adds to a few lines of memory come at the end of all workgroups at once.
 // 16 tokens 5.2 us; 30011 tokens of 60 fp32 experts, 4 of them, 7.7 us.
 // Workgroups of up to kRouteBlock threads; LDS: a token's words for each of its L threads, and a word per expert where tokens are counted.
 constexpr int kRouteBlock = 1024;
@@ -398,7 +403,7 @@ __global__ void __launch_bounds__(kRouteBlock) k_route(RouteParams P) {
                 across(std::integral_constant<int, 0x122>{});
                 across(std::integral_constant<int, 0x121>{});
                 if constexpr (L == 64) {
-                    top = larger(top, __shfl_xor(top, 16));
+                    top = larger(top, __shfl_xor(top, 16));  // (through LDS; an exchange of rows takes more instructions: 8 of 512 experts, 8 to a lane, 45 us against 42)
                     top = larger(top, __shfl_xor(top, 32));
                 }
                 if (l == r) e = expert_of(top);
@@ -515,6 +520,7 @@ static rtopk_status by_experts(int64_t experts, int64_t k, F&& f) {
         if (experts <= 64) return f(lanes, std::integral_constant<int, 4>{});
         if (experts <= 128) return f(lanes, std::integral_constant<int, 8>{});
         if (experts <= 256) return f(lanes, std::integral_constant<int, 16>{});
+        if (experts <= 512) return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 16>{});
     }
     std::integral_constant<int, 64> lanes;
     if (experts <= 256) return f(lanes, std::integral_constant<int, 4>{});
@@ -523,17 +529,17 @@ static rtopk_status by_experts(int64_t experts, int64_t k, F&& f) {
 }
 
 // f(how many of its best a lane keeps in order and merges with other lanes', or 0 where the best of the lanes' first is taken k times instead).  32768 bf16 tokens, merged / taken one by one,
-// us: of 256 experts 4: 13.7 / 18.3, 8: 16.4 / 22.5, 16: 21.5 / 31.2; of 1000 experts 8: 71 / 87, 16: 98 / 120; with fewer experts to a lane of 128 4: 9.9 / 10.4, 6: 12.4 / 11.4,
-// 10: 16.0 / 13.3; of 512 8: 47 / 42.
+// us: of 256 experts 4: 13.7 / 18.3, 8: 16.4 / 22.5, 16: 21.5 / 31.2; of 1000 experts 8: 67 / 87, 16: 94 / 120; with fewer experts to a lane of 128 4: 9.9 / 10.4, 6: 12.4 / 11.4,
+// 10: 16.0 / 13.3.
 template <int L, int N, class F>
 static rtopk_status by_choices(std::integral_constant<int, L>, std::integral_constant<int, N>, int64_t k, F&& f) {
     if constexpr (N == 16) {
         if (k <= 4) return f(std::integral_constant<int, 4>{});
         if (k <= 8) return f(std::integral_constant<int, 8>{});
-        if (L == 16 || k <= 16) return f(std::integral_constant<int, 16>{});
+        if (L < 64 || k <= 16) return f(std::integral_constant<int, 16>{});
     }
-    if constexpr (N != 16 || L != 16) return f(std::integral_constant<int, 0>{});
-    return RTOPK_ERR_INVALID_ARG;  // (16 lanes take 16 choices at most)
+    if constexpr (N != 16 || L == 64) return f(std::integral_constant<int, 0>{});
+    return RTOPK_ERR_INVALID_ARG;  // (fewer lanes take 16 choices at most)
 }
 
 }  // namespace rtopk
