@@ -57,6 +57,14 @@ __device__ __forceinline__ float finish_row(DistillRow& d, const SoftSum& a, con
     return rest != 0.0f ? rest * (kLn2 * log2_fast(rest) - ln_other) : 0.0f;
 }
 
+// Whether no earlier entry of a list has the i-th one's column.
+__device__ __forceinline__ bool is_first_of_column(const long long* columns, long long i) {
+    const long long t = columns[i];
+    for (long long j = 0; j < i; ++j)
+        if (columns[j] == t) return false;
+    return true;
+}
+
 // An entry's share under the teacher's log-sum, without the rounding of its logarithm: what all of them leave of 1 may be a millionth.
 __device__ __forceinline__ double exact_share(float z, float lse, float inv_t) {
     const float p = z * inv_t, low = __builtin_fmaf(z, inv_t, -p), hi = p - lse, back = hi - p;  // p + low is z inv_t exactly; hi + rest is p - lse exactly

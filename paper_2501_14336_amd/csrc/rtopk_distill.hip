@@ -30,11 +30,11 @@ struct RowList {
         if (e.t >= 0 && e.t < (long long)P.n) e.x = RowElem<DT>::load(r.x, (u32)e.t);
         return e;
     }
-    // f(entry, whether it is the first) for the thread's ones
+    // f(entry, its number) for the thread's ones
     template <int B, class F>
     __device__ __forceinline__ void each(F&& f) const {
-        if ((long long)threadIdx.x < P.k) f(first, true);
-        for (long long i = (long long)threadIdx.x + B; i < P.k; i += B) f(entry(i), false);
+        if ((long long)threadIdx.x < P.k) f(first, (long long)threadIdx.x);
+        for (long long i = (long long)threadIdx.x + B; i < P.k; i += B) f(entry(i), i);
     }
 };
 
@@ -50,7 +50,7 @@ __device__ __forceinline__ void loss_of_row(const DistillParams& P, long long ro
         d.zmul = 1.0f;
     } else {
         SoftSum z;
-        list.template each<B>([&](auto e, bool) {
+        list.template each<B>([&](auto e, long long) {
             if (e.t >= 0) {
                 const float v[1] = {e.z};
                 soft_add<false>(z, v, P.c);
@@ -65,7 +65,7 @@ __device__ __forceinline__ void loss_of_row(const DistillParams& P, long long ro
     const float ln_s = kLn2 * log2_fast(a.s);
     float loss = 0.0f;
     double share = 0.0;
-    list.template each<B>([&](auto e, bool) {
+    list.template each<B>([&](auto e, long long) {
         if (e.t < 0) return;
         const float lq = ln_share(e.z, d, TAIL, ln_zmul, P.inv_t), qi = expf(lq);
         if (TAIL) share += exact_share(e.z, d.zref, P.inv_t);
@@ -91,6 +91,7 @@ __global__ void __launch_bounds__(B) k_distill_part(DistillParams P) {
     extern __shared__ u32 marks[];  // TAIL: a byte per vector of the part, a bit per column
     __shared__ float4 sm[3][B / 64];
     __shared__ double sums[2 * B / 64];
+    __shared__ u32 twice;
     constexpr int E = RowElem<DT>::E, V = kDistillVecs;
     const u32 part = WHOLE ? 0u : blockIdx.x % P.parts;
     const long long row = P.row0 + (WHOLE ? blockIdx.x : blockIdx.x / P.parts);
@@ -101,25 +102,35 @@ __global__ void __launch_bounds__(B) k_distill_part(DistillParams P) {
     bool first_counts = false;
     if (TAIL) {
         for (u32 i = threadIdx.x; i < (P.part_vecs + 3) / 4; i += B) marks[i] = 0;
+        if (threadIdx.x == 0) twice = 0;
     }
     sweep_vectors<DT, B, V, NT>(r, v0, v1, [&](const u32x4 (&q)[V], u32 first) {
         if (TAIL && first == v0) {  // (with the first two tiles on their way)
             __syncthreads();
-            list.template each<B>([&](auto e, bool is_first) {
-                const u64 p = (u64)e.t + r.lead - (u64)v0 * E;  // (wraps below the part)
-                if (e.t >= 0 && e.t < (long long)P.n && p < (u64)(v1 - v0) * E) {
-                    const u32 v = (u32)p / E, bit = 1u << ((v & 3) * 8 + (u32)p % E);
-                    if (!(atomicOr(&marks[v >> 2], bit) & bit)) {  // a column listed twice counts once
-                        if (is_first) {
-                            first_counts = true;
-                        } else {
-                            const float x[1] = {e.x};
-                            soft_add<false>(listed, x, P.c);
-                        }
+            auto add_listed = [&](auto&& counts) {
+                list.template each<B>([&](auto e, long long i) {
+                    const u64 p = (u64)e.t + r.lead - (u64)v0 * E;  // (wraps below the part)
+                    if (e.t < 0 || e.t >= (long long)P.n || p >= (u64)(v1 - v0) * E || !counts((u32)p, i)) return;
+                    if (i == (long long)threadIdx.x) {
+                        first_counts = true;
+                    } else {
+                        const float x[1] = {e.x};
+                        soft_add<false>(listed, x, P.c);
                     }
-                }
+                });
+            };
+            add_listed([&](u32 p, long long) {
+                const u32 bit = 1u << ((p / E & 3) * 8 + p % E);
+                const bool again = (atomicOr(&marks[p / E >> 2], bit) & bit) != 0;
+                if (again) twice = 1;
+                return !again;
             });
             __syncthreads();
+            if (twice) {  // a column listed twice counts once, whichever thread came first: by its first entry
+                listed = SoftSum();
+                first_counts = false;
+                add_listed([&](u32, long long i) { return is_first_of_column(P.columns + list.from, i); });
+            }
         }
         float x[V * E];
 #pragma unroll

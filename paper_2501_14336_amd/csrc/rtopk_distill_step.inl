@@ -118,6 +118,18 @@ __global__ void __launch_bounds__(B, 4) k_distill_step(DistillParams P) {
                     soft_add<false>(listed, x, P.c);
                 }
             });
+        if (TAIL && list.repeated) {  // a column listed twice counts once, whichever thread came first: by its first entry
+            listed = SoftSum();
+#pragma unroll
+            for (int k = 0; k < R; ++k) list.fresh[k] = list.place[k] != list.kNone && is_first_of_column(columns, thread + (long long)k * B);
+#pragma clang loop unroll(disable)
+            for (long long i = thread + (long long)R * B; i < P.k; i += B) {
+                const long long t = columns[i];
+                if (t < 0 || t >= (long long)P.n || !is_first_of_column(columns, i)) continue;
+                const float x[1] = {RowElem<DT>::load(r.x, (u32)t)};
+                soft_add<false>(listed, x, P.c);
+            }
+        }
         // first pass: the softmax; TAIL: of what is not listed.  Listed columns' logits go to the threads that have their entries, by way of the tiles.  (Fetched by their columns they are a
         // line each: for 1024 of a row half as much again as the row.)
         SoftSum a;

@@ -178,3 +178,26 @@ def test_route_of_rows_off_the_grid_of_vectors(tokens, experts, k, dtype):
     into = out[:, 1:1 + experts]
     _ops().route_backward(x, at, w, out=into)
     assert torch.equal(into, _ops().route_backward(x, at, w)) and (out[:, 0] == 7).all() and (out[:, 1 + experts:] == 7).all()
+
+
+@pytest.mark.parametrize("tail", [False, True], ids=["list", "rest"])
+@pytest.mark.parametrize("batch,n,k", [(2, 150001, 900), (200, 3001, 700), (700, 2003, 300), (260, 9000, 1500)])
+def test_distill_columns_listed_more_than_once_give_the_same_bits_every_time(batch, n, k, tail):
+    ops = _ops()
+    x = _rows(batch, n, torch.float32, n)
+    g = torch.Generator(device="cuda").manual_seed(k)
+    indices = torch.randint(0, n, (batch, k), generator=g, device="cuda")
+    indices[:, k // 3:2 * (k // 3)] = indices[:, :k // 3].flip(1)
+    values = x.gather(1, indices) + torch.randn((batch, k), generator=g, device="cuda")
+    lse = torch.logsumexp(values.double(), 1).float() + 0.5 if tail else None
+    w = torch.rand((batch,), generator=g, device="cuda")
+
+    def all_of_it():
+        loss, stats = ops.distill(x, values, indices, lse)
+        return [loss, stats, ops.distill_backward(x, values, indices, stats, w, lse), *ops.distill_step(x, values, indices, w, lse)]
+
+    first = [t.clone() for t in all_of_it()]
+    for _ in range(4):
+        assert all(torch.equal(p, q) for p, q in zip(first, all_of_it()))
+    rows = slice(0, 4)
+    _check_distill(x[rows], values[rows], indices[rows], None if lse is None else lse[rows], 1.0)
