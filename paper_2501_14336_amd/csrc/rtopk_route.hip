@@ -261,7 +261,7 @@ __device__ __forceinline__ void best_two(u32& a, u32& b, u32 a2, u32 b2) {
 
 // Bound by instructions: for 256 experts to 16 lanes about 1700 a wave of four tokens, most of them for the scores (2^x and the reciprocal at a quarter of the rate), the keys and the order.
 // 16384 tokens of 256 bf16 experts, 8 of 4 of 8 groups, with a bias: 11.9 us, and 17.0 with the counts, whose adds to a few lines of memory come at the end of all workgroups at once.
-// 16 tokens 5.2 us; 30011 tokens of 60 fp32 experts, 4 of them, 7.7 us.
+// 16 tokens 5.3 us; 30011 tokens of 60 fp32 experts, 4 of them, 7.5 us.
 // Workgroups of up to kRouteBlock threads; LDS: a token's words for each of its L threads, and a word per expert where tokens are counted.
 constexpr int kRouteBlock = 1024;
 
@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kRouteBlock) k_route(RouteParams P) {
 
 // softmax:  dx_j = s_j (G_j - sum_l G_l s_l), or, renormalised, over the chosen alone with their shares in the place of s
 // sigmoid:  dx_j = G_j s_j (1 - s_j), with G = (g - sum_l g_l share_l) / sum s where it is renormalised
-// 30011 tokens of 60 fp32 experts 6.2 us, 2.4 TB/s; 32768 of 1000 fp32 67 us, 3.9 TB/s: bound by memory from there on, by instructions below.
+// 30011 tokens of 60 fp32 experts 6.1 us, 2.4 TB/s; 32768 of 1000 fp32 67 us, 3.9 TB/s: bound by memory from there on, by instructions below.
 constexpr int kRouteGradBlock = 256;
 
 template <int DT, int L, int N>

@@ -201,3 +201,52 @@ def test_distill_columns_listed_more_than_once_give_the_same_bits_every_time(bat
         assert all(torch.equal(p, q) for p, q in zip(first, all_of_it()))
     rows = slice(0, 4)
     _check_distill(x[rows], values[rows], indices[rows], None if lse is None else lse[rows], 1.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("tokens,experts,groups,topk_groups,k", [
+    (40, 400, 8, 3, 10), (33, 512, 32, 9, 4), (5000, 384, 12, 5, 6), (3, 257, 1, 1, 16), (50, 272, 17, 4, 3), (20, 160, 8, 3, 6), (4500, 240, 8, 4, 12), (6, 1024, 8, 4, 13),
+    (10, 960, 64, 20, 8), (7, 512, 8, 8, 33)])
+def test_route_groups_of_whole_lanes_and_others(tokens, experts, groups, topk_groups, k, dtype):
+    g = torch.Generator().manual_seed(experts + k)
+    x = (torch.randn((tokens, experts), generator=g) * 1.5).to(dtype).cuda()
+    bias = (torch.randn((experts,), generator=g) * 0.1).cuda()
+    kw = dict(groups=groups, topk_groups=topk_groups, scale=1.5)
+    _check_route(x, k, "softmax", **kw)
+    _check_route(x, k, "sigmoid", bias, group_score="top2" if experts // groups > 1 else "max", **kw)
+
+
+def test_route_scores_at_the_ends_of_the_range():
+    ops = _ops()
+    x = torch.full((6, 200), -math.inf, device="cuda")
+    x[0, 3], x[0, 9] = 200.0, -200.0                   # sigmoids of 1 and of less than any number
+    x[1, :50] = -87.5                                  # ... that are no ordinary numbers
+    x[2, 7] = math.inf
+    x[3] = 0.0
+    x[3, 5] = -88.0
+    x[4, :4] = torch.tensor([1e30, -1e30, 1e30, 0.0], device="cuda")
+    w, at = ops.route(x, 4, score="sigmoid", renormalize=False)
+    want = torch.sigmoid(x).gather(1, at)
+    assert torch.allclose(w, want, rtol=2e-6, atol=1e-44)
+    assert at[0, :2].tolist() == [3, 9] and at[1].tolist() == [0, 1, 2, 3] and at[5].tolist() == [0, 1, 2, 3] and not w[5].any()
+    w, at = ops.route(x, 4, score="softmax", renormalize=False)
+    assert w[2].isnan().any() and torch.allclose(w[[0, 1, 3, 4]], torch.softmax(x.double(), 1).gather(1, at)[[0, 1, 3, 4]].float(), rtol=2e-6, atol=1e-44)
+    assert not w[5].any()
+
+
+def test_route_counted_in_a_graph():
+    ops = _ops()
+    x = torch.randn((8200, 256), device="cuda").bfloat16()
+    bias = torch.randn((256,), device="cuda") * 0.1
+    counts = torch.zeros(256, dtype=torch.int64, device="cuda")
+    run = lambda c: ops.route(x, 8, score="sigmoid", bias=bias, groups=8, topk_groups=4, group_score="top2", counts=c)  # noqa: E731
+    eager = torch.zeros_like(counts)
+    w, at = run(eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = run(counts)
+    for i in range(1, 4):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held[0], w) and torch.equal(held[1], at) and torch.equal(counts, i * eager)
+        assert torch.equal(run(None)[1], at)
