@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(B) k_logprobs_sweep(LogprobsParams P) {
     if (threadIdx.x == 0) write_stats<W>(P, row, a, ln_s);
 }
 
-// A row's parts put together.  TOP: their lists too; otherwise the alternatives' values are there already (P.top_values).  4.8 us for 33 parts with 20 entries each (a launch that does
+// A row's parts put together.  TOP: their lists too; otherwise the alternatives' values are there already (P.top_values).  4.4 us for 33 parts with 20 entries each (a launch that does
 // nothing takes 2): one trip to what other units wrote, then ranks by comparisons in LDS.
 constexpr int kFinishBlock = 256;
 
@@ -378,7 +378,8 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         const u32 i = j * kFinishBlock + threadIdx.x;
-        e[j] = i < entries ? lists[i] : 0;
+        e[j] = 0;
+        if (j * kFinishBlock < entries) e[j] = i < entries ? lists[i] : 0;
     }
     SoftSum a;
     for (u32 i = threadIdx.x; i < P.parts; i += kFinishBlock) a = soft_join<W>(a, unpacked(P.partial[row * P.parts + i]), P.c);
@@ -406,7 +407,7 @@ __global__ void __launch_bounds__(kFinishBlock) k_logprobs_finish(LogprobsParams
         const u64 bound = top.bound64;
 #pragma unroll
         for (int j = 0; j < kEach; ++j)
-            if (e[j] >= bound && e[j] != 0) {
+            if (j * kFinishBlock < entries && e[j] >= bound && e[j] != 0) {
                 const u32 place = atomicAdd(&top.count, 1u);
                 if (place < kListRoom) top.list[place] = e[j];
             }
